@@ -1,4 +1,4 @@
-"""Build libjq.so (the gfx950 HIP library behind include/jq.h) in-tree with hipcc.
+"""Build libjq.so (the gfx950 HIP library behind include/jq.h and jq_block.h) in-tree with hipcc.
 
 Each source compiles to its own object in parallel (_build/), then one hipcc
 link makes the shared library.  Every call compiles every source.  Alongside,
@@ -24,7 +24,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libjq.so")
 SOURCES = ["quantize.hip", "ternary.hip", "gemm.hip", "gemm_narrow.hip", "gemm_wide.hip", "gemm_group.hip", "f6.hip",
-           "f6_narrow.hip", "f6_narrow_group.hip", "f6_quant_few.hip", "jq_api.cpp"]
+           "f6_narrow.hip", "f6_narrow_group.hip", "f6_quant_few.hip", "jq_api.cpp", "rmsnorm.hip", "fp8_quant.hip",
+           "fp8_gemm.hip", "rope_append.hip", "paged_attention.hip", "jq_block_api.cpp"]
 ARCH = "gfx950"
 
 # Per-source flags: the BF6 kernels are built without machine sinking, which

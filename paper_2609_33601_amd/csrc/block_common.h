@@ -1,0 +1,121 @@
+// Device helpers shared by the kernels of a decoder block's other operators
+// (norm, 8-bit linear, rotation with paged append, paged attention): bf16 and
+// e4m3 conversions, scales, and reductions inside a wave.  Device code only.
+#ifndef JQ_BLOCK_COMMON_H
+#define JQ_BLOCK_COMMON_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace jq {
+namespace block_detail {
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ float bf_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// Two floats rounded to bf16 (nearest even), the first in the low half.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const bf16x2 v = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+__device__ __forceinline__ void unpack8_bf16(u32x4 u, float* f) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f[2 * j] = bf_lo(u[j]);
+    f[2 * j + 1] = bf_hi(u[j]);
+  }
+}
+
+__device__ __forceinline__ u32x4 pack8_bf16(const float* f) {
+  return u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+}
+
+// Eight floats rounded to e4m3 (nearest even; NaN stays NaN).
+__device__ __forceinline__ u32x2 pack8_e4m3(const float* f) {
+  u32x2 r;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * j], f[4 * j + 1], 0, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * j + 2], f[4 * j + 3], v, true);
+    r[j] = static_cast<uint32_t>(v);
+  }
+  return r;
+}
+
+// The scale of values whose largest magnitude has these bits: a / 448, at
+// least 2^-126 so that its reciprocal is finite; 0 where all are 0.  Bits of
+// magnitudes order like the magnitudes with NaN on top, so an infinity or NaN
+// among the values makes the scale one, and every product with it too.
+__device__ __forceinline__ float e4m3_scale(uint32_t amax_bits) {
+  float s = __uint_as_float(amax_bits) / 448.0f;
+  if (s < 0x1p-126f) s = amax_bits == 0 ? 0.0f : 0x1p-126f;
+  return s;
+}
+__device__ __forceinline__ float e4m3_inv(float s) { return s == 0.0f ? 0.0f : 1.0f / s; }
+
+// fl32(v / s) from inv = fl32(1 / s), three operations instead of a division's
+// ten: the remainder of v * inv is exact in one fma, and adding it times inv
+// rounds correctly because inv is the rounded reciprocal (Markstein).  bf16
+// inputs meet ties of e4m3 too often for a quotient that is an ulp off.
+__device__ __forceinline__ float e4m3_quotient(float v, float s, float inv) {
+  const float q = v * inv;
+  return fmaf(fmaf(-q, s, v), inv, q);
+}
+
+// The value of another lane of the same row of 16 (DPP), all lanes taking part.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+
+// Largest value of L neighbouring lanes (L = 2, 4, 8, 16, 32), left in each.
+template <int L>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  if constexpr (L >= 2) v = umax(v, dpp<kDppXor1>(v));
+  if constexpr (L >= 4) v = umax(v, dpp<kDppXor2>(v));
+  if constexpr (L >= 8) v = umax(v, dpp<kDppHalfMirror>(v));
+  if constexpr (L >= 16) v = umax(v, dpp<kDppMirror>(v));
+  if constexpr (L >= 32) v = umax(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16, 64)));
+  return v;
+}
+
+// Sum over L neighbouring lanes (L = 8, 16, 32, 64), left in each, in an order
+// that does not depend on the lane.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  auto f = [](uint32_t u) { return __uint_as_float(u); };
+  auto u = [](float x) { return __float_as_uint(x); };
+  v += f(dpp<kDppXor1>(u(v)));
+  v += f(dpp<kDppXor2>(u(v)));
+  v += f(dpp<kDppHalfMirror>(u(v)));
+  if constexpr (L >= 16) v += f(dpp<kDppMirror>(u(v)));
+  if constexpr (L == 32) v += __shfl_xor(v, 16, 64);
+  if constexpr (L == 64) {
+    const int i = static_cast<int>(u(v));
+    v = (f(__builtin_amdgcn_readlane(i, 0)) + f(__builtin_amdgcn_readlane(i, 16))) +
+        (f(__builtin_amdgcn_readlane(i, 32)) + f(__builtin_amdgcn_readlane(i, 48)));
+  }
+  return v;
+}
+
+// Largest of a wave, uniform.
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
+  const int i = static_cast<int>(lanes_max<16>(v));
+  return umax(umax(static_cast<uint32_t>(__builtin_amdgcn_readlane(i, 0)), static_cast<uint32_t>(__builtin_amdgcn_readlane(i, 16))),
+              umax(static_cast<uint32_t>(__builtin_amdgcn_readlane(i, 32)), static_cast<uint32_t>(__builtin_amdgcn_readlane(i, 48))));
+}
+
+}  // namespace block_detail
+}  // namespace jq
+
+#endif  // JQ_BLOCK_COMMON_H
