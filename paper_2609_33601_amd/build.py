@@ -26,6 +26,9 @@ LIB = os.path.join(PKG, "libjq.so")
 SOURCES = ["quantize.hip", "ternary.hip", "gemm.hip", "gemm_narrow.hip", "gemm_wide.hip", "gemm_group.hip", "f6.hip",
            "f6_narrow.hip", "f6_narrow_group.hip", "f6_quant_few.hip", "jq_api.cpp", "rmsnorm.hip", "fp8_quant.hip",
            "fp8_gemm.hip", "rope_append.hip", "paged_attention.hip", "jq_block_api.cpp"]
+# The compiled half of the binding of jq_block.h: a Python extension on torch's C++ headers.
+BINDING_SOURCE = "jq_block_py.cpp"
+BINDING = os.path.join(PKG, "_jq_block.so")
 ARCH = "gfx950"
 
 # Per-source flags: the BF6 kernels are built without machine sinking, which
@@ -88,7 +91,26 @@ def build(verbose=False, extra_flags=(), jobs=None):
     tmp = LIB + ".tmp"
     _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp], verbose)
     os.replace(tmp, LIB)
+    build_binding(verbose)
     return LIB
+
+
+def build_binding(verbose=False):
+    """Compile jq_block.py's extension against the built libjq.so."""
+    import sysconfig
+
+    from torch.utils import cpp_extension
+
+    rocm = os.path.dirname(os.path.dirname(hipcc()))
+    dirs = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(rocm, "include"),
+                                            os.path.join(ROOT, "include")]
+    tmp = BINDING + ".tmp"
+    _run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+          "-DUSE_ROCM", *[a for d in dirs for a in ("-isystem", d)], os.path.join(CSRC, BINDING_SOURCE), "-o", tmp,
+          "-L", PKG, "-ljq", *[a for d in cpp_extension.library_paths() for a in ("-L", d)],
+          "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], verbose)
+    os.replace(tmp, BINDING)
+    return BINDING
 
 
 if __name__ == "__main__":
