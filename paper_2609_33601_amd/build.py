@@ -31,9 +31,10 @@ BINDING_SOURCE = "jq_block_py.cpp"
 BINDING = os.path.join(PKG, "_jq_block.so")
 ARCH = "gfx950"
 
-# Per-source flags: the BF6 kernels are built without machine sinking, which
-# would move the first k-step's MFMAs of a GEMM stage below its barrier.
-SOURCE_FLAGS = {"f6.hip": ["-mllvm", "-disable-machine-sink"]}
+# Per-source flags: the BF6 and 8-bit GEMMs are built without machine sinking, which
+# would move the first k-step's MFMAs of a BF6 stage below its barrier, and the
+# multiply-adds of an 8-bit stage behind all of its MFMAs (100 registers spilled).
+SOURCE_FLAGS = {"f6.hip": ["-mllvm", "-disable-machine-sink"], "fp8_gemm.hip": ["-mllvm", "-disable-machine-sink"]}
 # Sources whose asm-issued loads are checked against their waits, and the
 # kernel names checked in each.
 CHECKED_SOURCES = {"f6.hip": "w4a4_f6_gemm_kernel"}

@@ -139,21 +139,37 @@ __global__ __launch_bounds__(64 * WM * WN, PER_CU) void fp8_gemm_kernel(
     }
     const uint4* xs = lds + cur * kStage;
     const uint4* ws = xs + BM * 8;
+    const int row0 = wm * (BM / WM) + li;
     i32x8 w[kFN];
 #pragma unroll
     for (int a = 0; a < kFN; ++a) w[a] = frag(ws, wn * (BN / WN) + 16 * a + li);
     const float swv = swp[ks];
+    // Row group b multiplies while b - 1 is folded and b + 1 is read.
+    i32x8 x = frag(xs, row0);
+    float s = sxl[cur * BM + row0] * swv;
+    float sp = 0.0f;
+    f32x4 p[kFN];
 #pragma unroll
-    for (int b = 0; b < kFM; ++b) {
-      const int row = wm * (BM / WM) + 16 * b + li;
-      const i32x8 x = frag(xs, row);
-      const float s = sxl[cur * BM + row] * swv;
+    for (int b = 0; b <= kFM; ++b) {
+      i32x8 xn = x;
+      float sn = s;
+      if (b + 1 < kFM) {
+        xn = frag(xs, row0 + 16 * (b + 1));
+        sn = sxl[cur * BM + row0 + 16 * (b + 1)] * swv;
+      }
+      f32x4 q[kFN];
 #pragma unroll
       for (int a = 0; a < kFN; ++a) {
-        const f32x4 p = mfma128(w[a], x);
+        if (b < kFM) q[a] = mfma128(w[a], x);
+        if (b > 0) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[a][b][r] = fmaf(p[r], s, acc[a][b][r]);
+          for (int r = 0; r < 4; ++r) acc[a][b - 1][r] = fmaf(p[a][r], sp, acc[a][b - 1][r]);
+        }
       }
+#pragma unroll
+      for (int a = 0; a < kFN; ++a) p[a] = q[a];
+      sp = s, x = xn, s = sn;
+      __builtin_amdgcn_sched_barrier(0);
     }
     if (tid < BM) sxl[(cur ^ 1) * BM + tid] = sx_next;
   }
