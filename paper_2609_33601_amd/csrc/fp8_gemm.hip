@@ -20,7 +20,6 @@ namespace jq {
 namespace {
 
 using namespace block_detail;
-using gemm_detail::dma16;
 using gemm_detail::kBufferFlags;
 using gemm_detail::kNumXcd;
 using gemm_detail::kOutsideOperand;
@@ -40,20 +39,55 @@ __device__ __forceinline__ f32x4 mfma128(i32x8 w, i32x8 x) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
 }
 
-__device__ __forceinline__ void store4(uint16_t* y, int64_t row, int N, int n, f32x4 v, const uint16_t* bias) {
-  float f[4];
+// Transfers from a buffer into LDS, 16 (or 4) bytes per lane: lane i writes
+// lds + 16 i (4 i).  As asm, because the compiler waits for transfers that it
+// knows of before the next LDS read, whatever part of LDS that reads, and the
+// whole point of two stages is not to.  The kernel waits itself (vmcnt(0) at
+// the head of a stage).  The wait states that the compiler would put behind the
+// writes of M0 and of descriptor words are in the asm; the build checks them.
+typedef unsigned u32x4s __attribute__((ext_vector_type(4)));
+struct Rsrc {
+  u32x4s w;
+};
+__device__ __forceinline__ Rsrc make_rsrc(const void* base, int bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32)) & 0xFFFFu;
+  const uint32_t n = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(bytes));
+  return {u32x4s{lo, hi, n, static_cast<uint32_t>(kBufferFlags)}};
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
+}
+__device__ __forceinline__ void dma16(const Rsrc& r, uint32_t lds, uint32_t voffset, uint32_t soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voffset), "s"(r.w), "s"(soffset)
+               : "memory");
+}
+__device__ __forceinline__ void dma4(const Rsrc& r, uint32_t lds, uint32_t voffset, uint32_t soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voffset), "s"(r.w), "s"(soffset)
+               : "memory");
+}
+
+// Four columns' bias, zeros where there is none.
+__device__ __forceinline__ f32x4 bias4(const uint16_t* bias, int n, int N) {
+  f32x4 v = {0, 0, 0, 0};
+  if (bias != nullptr) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    f[r] = v[r];
-    if (bias != nullptr) f[r] = f[r] + bf_lo(bias[min(n + r, N - 1)]);
+    for (int r = 0; r < 4; ++r) v[r] = bf_lo(bias[min(n + r, N - 1)]);
   }
+  return v;
+}
+
+__device__ __forceinline__ void store4(uint16_t* y, int64_t row, int N, int n, f32x4 v) {
   uint16_t* p = y + row * N + n;
-  if (N % 4 == 0 && n + 4 <= N) {
-    *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
+  if (N % 4 == 0) {
+    *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (n + r < N) p[r] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(f[r]));
+      if (n + r < N) p[r] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[r]));
   }
 }
 
@@ -87,31 +121,30 @@ __global__ __launch_bounds__(64 * WM * WN, PER_CU) void fp8_gemm_kernel(
   const int kb = (K + 127) / 128;
 
   // Descriptors over this tile's rows only, so operands of any size have 32-bit offsets.
-  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(qx) + static_cast<int64_t>(m0) * K, 0, min(BM, M - m0) * K, kBufferFlags);
-  const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(qw) + static_cast<int64_t>(n0) * K, 0, min(BN, N - n0) * K, kBufferFlags);
+  const Rsrc rx = make_rsrc(qx + static_cast<int64_t>(m0) * K, min(BM, M - m0) * K);
+  const Rsrc rw = make_rsrc(qw + static_cast<int64_t>(n0) * K, min(BN, N - n0) * K);
+  const Rsrc rs = make_rsrc(sx + static_cast<int64_t>(m0) * kb, min(BM, M - m0) * kb * 4);
   // Lane l of a DMA fills slot l % 8 of row l / 8.  Rows past M or N, and
   // chunks past K, have offsets outside the descriptor and read as zero.
   const int chunk = (lane & 7) ^ (lane >> 3);
+  const uint32_t lds0 = lds_addr(lds), sxl0 = lds_addr(sxl);
   auto issue = [&](int stage, int ks) __attribute__((always_inline)) {
-    uint4* buf = lds + stage * kStage;
-    const bool in = ks * 128 + 16 * chunk < K;
+    const uint32_t buf = lds0 + stage * kStage * 16;
+    const uint32_t at = ks * 128 + 16 * chunk < K ? 16 * chunk : kOutsideOperand;
 #pragma unroll
     for (int j = 0; j < kXDma; ++j) {
       const int r = 8 * (wave * kXDma + j) + (lane >> 3);
-      dma16(rx, buf + 64 * (wave * kXDma + j), in ? r * K + 16 * chunk : kOutsideOperand, ks * 128);
+      dma16(rx, buf + 1024 * (wave * kXDma + j), r * K + at, ks * 128);
     }
 #pragma unroll
     for (int j = 0; j < kWDma; ++j) {
       const int r = 8 * (wave * kWDma + j) + (lane >> 3);
-      dma16(rw, buf + BM * 8 + 64 * (wave * kWDma + j), in ? r * K + 16 * chunk : kOutsideOperand, ks * 128);
+      dma16(rw, buf + BM * 128 + 1024 * (wave * kWDma + j), r * K + at, ks * 128);
     }
+    if (wave < BM / 64) dma4(rs, sxl0 + 4 * (stage * BM + 64 * wave), (64 * wave + lane) * kb * 4, ks * 4);
   };
-  const float* swp = sw + static_cast<int64_t>((n0 + wn * (BN / WN)) / 128 < (N + 127) / 128 ? (n0 + wn * (BN / WN)) / 128 : 0) * kb;
-  auto load_sx = [&](int ks) __attribute__((always_inline)) -> float {
-    return tid < BM && m0 + tid < M ? sx[static_cast<int64_t>(m0 + tid) * kb + ks] : 0.0f;
-  };
+  const int nb = min((n0 + wn * (BN / WN)) / 128, (N - 1) / 128);
+  const float* swp = sw + static_cast<int64_t>(nb) * kb;
 
   f32x4 acc[kFN][kFM];
 #pragma unroll
@@ -121,29 +154,26 @@ __global__ __launch_bounds__(64 * WM * WN, PER_CU) void fp8_gemm_kernel(
 
   auto frag = [&](const uint4* rows, int row) __attribute__((always_inline)) -> i32x8 {
     const int s = row & 7;
-    const u32x4 lo = __builtin_bit_cast(u32x4, rows[row * 8 + ((2 * lg) ^ s)]);
-    const u32x4 hi = __builtin_bit_cast(u32x4, rows[row * 8 + ((2 * lg + 1) ^ s)]);
+    // lane group lg takes chunks lg and 4 + lg (any k order serves, the same on both sides)
+    const u32x4 lo = __builtin_bit_cast(u32x4, rows[row * 8 + (lg ^ s)]);
+    const u32x4 hi = __builtin_bit_cast(u32x4, rows[row * 8 + ((4 + lg) ^ s)]);
     return join_regs(lo, hi);
   };
 
   issue(0, 0);
-  if (tid < BM) sxl[tid] = load_sx(0);
+  float swv = swp[0];
   for (int ks = 0; ks < kb; ++ks) {
     const int cur = ks & 1;
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    float sx_next = 0.0f;
-    if (ks + 1 < kb) {
-      issue(cur ^ 1, ks + 1);
-      sx_next = load_sx(ks + 1);
-    }
+    if (ks + 1 < kb) issue(cur ^ 1, ks + 1);
+    const float sw_next = swp[min(ks + 1, kb - 1)];
     const uint4* xs = lds + cur * kStage;
     const uint4* ws = xs + BM * 8;
     const int row0 = wm * (BM / WM) + li;
     i32x8 w[kFN];
 #pragma unroll
     for (int a = 0; a < kFN; ++a) w[a] = frag(ws, wn * (BN / WN) + 16 * a + li);
-    const float swv = swp[ks];
     // Row group b multiplies while b - 1 is folded and b + 1 is read.
     i32x8 x = frag(xs, row0);
     float s = sxl[cur * BM + row0] * swv;
@@ -171,16 +201,18 @@ __global__ __launch_bounds__(64 * WM * WN, PER_CU) void fp8_gemm_kernel(
       sp = s, x = xn, s = sn;
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (tid < BM) sxl[(cur ^ 1) * BM + tid] = sx_next;
+    swv = sw_next;
   }
 
 #pragma unroll
-  for (int b = 0; b < kFM; ++b) {
-    const int m = m0 + wm * (BM / WM) + 16 * b + li;
+  for (int a = 0; a < kFN; ++a) {
+    const int n = n0 + wn * (BN / WN) + 16 * a + 4 * lg;
+    if (n >= N) continue;
+    const f32x4 bv = bias4(bias, n, N);
 #pragma unroll
-    for (int a = 0; a < kFN; ++a) {
-      const int n = n0 + wn * (BN / WN) + 16 * a + 4 * lg;
-      if (m < M && n < N) store4(y, m, N, n, acc[a][b], bias);
+    for (int b = 0; b < kFM; ++b) {
+      const int m = m0 + wm * (BM / WM) + 16 * b + li;
+      if (m < M) store4(y, m, N, n, acc[a][b] + bv);
     }
   }
 }
@@ -256,7 +288,7 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
 #pragma unroll
         for (int k = 1; k < W; ++k) v += red[k * 64 + lane];
         const int m = m0 + 16 * b + li, n = n0 + 16 * a + 4 * lg;
-        if (m < M && n < N) store4(y, m, N, n, v, bias);
+        if (m < M && n < N) store4(y, m, N, n, v + bias4(bias, n, N));
       }
     }
 }
