@@ -11,6 +11,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "block_common.h"
 #include "block_internal.h"
 #include "gemm_common.h"
@@ -70,6 +73,14 @@ __device__ __forceinline__ void dma4(const Rsrc& r, uint32_t lds, uint32_t voffs
                : "memory");
 }
 
+// Tile t in the grouped order of tile_of_block: 8 tiles of m per sweep of n.
+__device__ __forceinline__ TileCoord tile_at(int t, int tiles_m, int tiles_n) {
+  constexpr int kGroup = gemm_detail::kGroupM;
+  const int group = t / (kGroup * tiles_n), first_m = group * kGroup;
+  const int gm = min(tiles_m - first_m, kGroup), r = t - group * kGroup * tiles_n;
+  return {first_m + r % gm, r / gm};
+}
+
 // Four columns' bias, zeros where there is none.
 __device__ __forceinline__ f32x4 bias4(const uint16_t* bias, int n, int N) {
   f32x4 v = {0, 0, 0, 0};
@@ -93,127 +104,215 @@ __device__ __forceinline__ void store4(uint16_t* y, int64_t row, int N, int n, f
 
 // ---------------------------------------------------------------------------
 // Many output tiles.  A block takes BM x BN outputs, WM x WN waves of it
-// 16 FM x 16 FN each; stages of one block of 128 k, two in LDS, both operands
-// moved by buffer-to-LDS DMA.  LDS rows are 128 bytes; the 16-byte chunk c of
-// row r sits at slot c ^ (r & 7), so the sixteen rows that a fragment read
-// spans cover all banks.
+// 16 FM x 16 FN each, and walks a sequence of tiles as one sequence of stages
+// of 128 k.  Both operands come by buffer-to-LDS transfers, two stages in LDS.
+// LDS rows are 128 bytes; the 16-byte chunk c of row r sits at slot
+// c ^ (r & 7), so that the sixteen rows a fragment read spans cover all banks.
+//
+// The one barrier of a stage stands before its last two row groups, whose
+// operands are in registers by then: behind it the stage's buffer is free for
+// the transfers of the stage after next, and the next stage's weights and first
+// row group are read while the two groups multiply.  Between stages, and
+// between tiles, the matrix pipe sees no gap but the stores.
 
-template <int BM, int BN, int WM, int WN, int PER_CU>
-__global__ __launch_bounds__(64 * WM * WN, PER_CU) void fp8_gemm_kernel(
+template <int BM, int BN, int WM, int WN, int WPS>
+__global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
     const uint8_t* __restrict__ qx, const float* __restrict__ sx, int M, int K, const uint8_t* __restrict__ qw,
     const float* __restrict__ sw, int N, const uint16_t* __restrict__ bias, uint16_t* __restrict__ y, int tiles_m,
     int tiles_n) {
   constexpr int kWaves = WM * WN;
   constexpr int kFM = BM / WM / 16, kFN = BN / WN / 16;
-  constexpr int kXDma = BM / 8 / kWaves, kWDma = BN / 8 / kWaves;  // DMA instructions per wave and stage: 8 rows each
+  constexpr int kXDma = BM / 8 / kWaves, kWDma = BN / 8 / kWaves;  // transfers per wave and stage: 8 rows each
   constexpr int kStage = (BM + BN) * 8;                            // 16-byte slots
   static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && 128 % (BN / WN) == 0, "");
+  static_assert(kFN == 4 && kFM >= 4 && BM / 64 <= kWaves, "");
   __shared__ uint4 lds[2 * kStage];
   __shared__ float sxl[2 * BM];
 
-  TileCoord tc;
-  if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, &tc)) return;
-  const int m0 = tc.tm * BM, n0 = tc.tn * BN;
+  // XCD x takes a contiguous range of tiles, its blocks in turn.
+  const int T = tiles_m * tiles_n, per_xcd = (T + kNumXcd - 1) / kNumXcd;
+  const int step = gridDim.x / kNumXcd, xcd = blockIdx.x % kNumXcd;
+  const int first = xcd * per_xcd + blockIdx.x / kNumXcd, end = min((xcd + 1) * per_xcd, T);
+  if (first >= end) return;
+  const int kb = (K + 127) / 128;
+  const int stages = ((end - 1 - first) / step + 1) * kb;
+
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
   const int li = lane & 15, lg = lane >> 4;
-  const int kb = (K + 127) / 128;
-
-  // Descriptors over this tile's rows only, so operands of any size have 32-bit offsets.
-  const Rsrc rx = make_rsrc(qx + static_cast<int64_t>(m0) * K, min(BM, M - m0) * K);
-  const Rsrc rw = make_rsrc(qw + static_cast<int64_t>(n0) * K, min(BN, N - n0) * K);
-  const Rsrc rs = make_rsrc(sx + static_cast<int64_t>(m0) * kb, min(BM, M - m0) * kb * 4);
-  // Lane l of a DMA fills slot l % 8 of row l / 8.  Rows past M or N, and
-  // chunks past K, have offsets outside the descriptor and read as zero.
-  const int chunk = (lane & 7) ^ (lane >> 3);
   const uint32_t lds0 = lds_addr(lds), sxl0 = lds_addr(sxl);
-  auto issue = [&](int stage, int ks) __attribute__((always_inline)) {
-    const uint32_t buf = lds0 + stage * kStage * 16;
-    const uint32_t at = ks * 128 + 16 * chunk < K ? 16 * chunk : kOutsideOperand;
-#pragma unroll
-    for (int j = 0; j < kXDma; ++j) {
-      const int r = 8 * (wave * kXDma + j) + (lane >> 3);
-      dma16(rx, buf + 1024 * (wave * kXDma + j), r * K + at, ks * 128);
-    }
-#pragma unroll
-    for (int j = 0; j < kWDma; ++j) {
-      const int r = 8 * (wave * kWDma + j) + (lane >> 3);
-      dma16(rw, buf + BM * 128 + 1024 * (wave * kWDma + j), r * K + at, ks * 128);
-    }
-    if (wave < BM / 64) dma4(rs, sxl0 + 4 * (stage * BM + 64 * wave), (64 * wave + lane) * kb * 4, ks * 4);
+
+  // Transfers run two stages ahead of the products: their own tile and stage.
+  // Descriptors cover a tile's rows only, so operands of any size have 32-bit
+  // offsets; rows past M or N, and chunks past K, have offsets outside the
+  // descriptor and read as zero.  Lane l of a transfer fills slot l % 8 of row l / 8.
+  const int chunk = (lane & 7) ^ (lane >> 3);
+  int to = first, ks_to = 0, left = stages;
+  Rsrc rx, rw, rs;
+  auto aim = [&]() __attribute__((always_inline)) {
+    const TileCoord tc = tile_at(to, tiles_m, tiles_n);
+    const int m0 = tc.tm * BM, n0 = tc.tn * BN;
+    rx = make_rsrc(qx + static_cast<int64_t>(m0) * K, min(BM, M - m0) * K);
+    rw = make_rsrc(qw + static_cast<int64_t>(n0) * K, min(BN, N - n0) * K);
+    rs = make_rsrc(sx + static_cast<int64_t>(m0) * kb, min(BM, M - m0) * kb * 4);
   };
-  const int nb = min((n0 + wn * (BN / WN)) / 128, (N - 1) / 128);
-  const float* swp = sw + static_cast<int64_t>(nb) * kb;
+  auto issue = [&](int buf) __attribute__((always_inline)) {
+    if (left == 0) return;
+    --left;
+    const uint32_t dst = lds0 + buf * kStage * 16;
+    const uint32_t at = ks_to * 128 + 16 * chunk < K ? 16 * chunk + (lane >> 3) * K : kOutsideOperand;
+#pragma unroll
+    for (int j = 0; j < kXDma; ++j)
+      dma16(rx, dst + 1024 * (wave * kXDma + j), 8 * (wave * kXDma + j) * K + at, ks_to * 128);
+#pragma unroll
+    for (int j = 0; j < kWDma; ++j)
+      dma16(rw, dst + BM * 128 + 1024 * (wave * kWDma + j), 8 * (wave * kWDma + j) * K + at, ks_to * 128);
+    if (wave < BM / 64) dma4(rs, sxl0 + 4 * (buf * BM + 64 * wave), (64 * wave + lane) * kb * 4, ks_to * 4);
+    if (++ks_to == kb) {
+      ks_to = 0;
+      to += step;
+      if (left > 0) aim();
+    }
+  };
 
   f32x4 acc[kFN][kFM];
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int a = 0; a < kFN; ++a)
+    for (int a = 0; a < kFN; ++a)
 #pragma unroll
-    for (int b = 0; b < kFM; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
-
+      for (int b = 0; b < kFM; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
+  };
   auto frag = [&](const uint4* rows, int row) __attribute__((always_inline)) -> i32x8 {
-    const int s = row & 7;
     // lane group lg takes chunks lg and 4 + lg (any k order serves, the same on both sides)
+    const int s = row & 7;
     const u32x4 lo = __builtin_bit_cast(u32x4, rows[row * 8 + (lg ^ s)]);
     const u32x4 hi = __builtin_bit_cast(u32x4, rows[row * 8 + ((4 + lg) ^ s)]);
     return join_regs(lo, hi);
   };
+  const int xrow = wm * (BM / WM) + li, wrow = wn * (BN / WN) + li;
+  auto x_at = [&](int buf, int b) __attribute__((always_inline)) { return frag(lds + buf * kStage, xrow + 16 * b); };
+  auto w_at = [&](int buf, int a) __attribute__((always_inline)) { return frag(lds + buf * kStage + BM * 8, wrow + 16 * a); };
+  auto s_at = [&](int buf, int b) __attribute__((always_inline)) { return sxl[buf * BM + xrow + 16 * b]; };
 
-  issue(0, 0);
-  float swv = swp[0];
-  for (int ks = 0; ks < kb; ++ks) {
-    const int cur = ks & 1;
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-    if (ks + 1 < kb) issue(cur ^ 1, ks + 1);
-    const float sw_next = swp[min(ks + 1, kb - 1)];
-    const uint4* xs = lds + cur * kStage;
-    const uint4* ws = xs + BM * 8;
-    const int row0 = wm * (BM / WM) + li;
-    i32x8 w[kFN];
+  // The tile being multiplied, and its weights' scales.
+  int at = first, ks = 0;
+  TileCoord tc = tile_at(at, tiles_m, tiles_n);
+  auto scales = [&]() __attribute__((always_inline)) {
+    const float* p = sw + static_cast<int64_t>(min((tc.tn * BN + wn * (BN / WN)) / 128, (N - 1) / 128)) * kb;
+    return (const __attribute__((address_space(4))) float*)p;
+  };
+  // read with scalar loads: a vector load's wait would take in the transfers under way
+  typedef const __attribute__((address_space(4))) float* uniform_f32;
+  uniform_f32 swp = scales();
+
+  auto store = [&]() __attribute__((always_inline)) {
+    const int m0 = tc.tm * BM + xrow, n0 = tc.tn * BN + wn * (BN / WN);
+    if (N % 8 == 0 && n0 + 64 <= N) {
+      // Lane group lg holds columns 16 a + 4 lg ..; swapping registers between
+      // groups gives it 8 consecutive ones of each 32, so that a store covers
+      // 64 consecutive bytes of each of 16 rows instead of 32.
 #pragma unroll
-    for (int a = 0; a < kFN; ++a) w[a] = frag(ws, wn * (BN / WN) + 16 * a + li);
-    // Row group b multiplies while b - 1 is folded and b + 1 is read.
-    i32x8 x = frag(xs, row0);
-    float s = sxl[cur * BM + row0] * swv;
-    float sp = 0.0f;
-    f32x4 p[kFN];
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 b0 = bias4(bias, n0 + 32 * h + 4 * lg, N), b1 = bias4(bias, n0 + 32 * h + 16 + 4 * lg, N);
 #pragma unroll
-    for (int b = 0; b <= kFM; ++b) {
-      i32x8 xn = x;
-      float sn = s;
-      if (b + 1 < kFM) {
-        xn = frag(xs, row0 + 16 * (b + 1));
-        sn = sxl[cur * BM + row0 + 16 * (b + 1)] * swv;
-      }
-      f32x4 q[kFN];
+        for (int b = 0; b < kFM; ++b) {
+          const f32x4 v0 = acc[2 * h][b] + b0, v1 = acc[2 * h + 1][b] + b1;
+          u32x4 out;
 #pragma unroll
-      for (int a = 0; a < kFN; ++a) {
-        if (b < kFM) q[a] = mfma128(w[a], x);
-        if (b > 0) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[a][b - 1][r] = fmaf(p[a][r], sp, acc[a][b - 1][r]);
+          for (int i = 0; i < 2; ++i) {
+            const auto r = __builtin_amdgcn_permlane32_swap(pack_bf16(v0[2 * i], v0[2 * i + 1]),
+                                                            pack_bf16(v1[2 * i], v1[2 * i + 1]), false, false);
+            const auto q = __builtin_amdgcn_permlane16_swap(r[0], r[1], false, false);
+            out[i] = q[0], out[2 + i] = q[1];
+          }
+          const int m = m0 + 16 * b;
+          if (m < M) *reinterpret_cast<u32x4*>(y + static_cast<int64_t>(m) * N + n0 + 32 * h + 8 * lg) = out;
         }
       }
+    } else {
 #pragma unroll
-      for (int a = 0; a < kFN; ++a) p[a] = q[a];
-      sp = s, x = xn, s = sn;
-      __builtin_amdgcn_sched_barrier(0);
+      for (int a = 0; a < kFN; ++a) {
+        const int n = n0 + 16 * a + 4 * lg;
+        if (n >= N) continue;
+        const f32x4 bv = bias4(bias, n, N);
+#pragma unroll
+        for (int b = 0; b < kFM; ++b)
+          if (m0 + 16 * b < M) store4(y, m0 + 16 * b, N, n, acc[a][b] + bv);
+      }
     }
-    swv = sw_next;
-  }
+  };
 
+  i32x8 w[2][kFN], x0;  // this stage's weights and the next one's; a stage's first row group
+  float s0, swv = swp[0];
+  auto stage = [&](auto B_) __attribute__((always_inline)) {
+    constexpr int B = decltype(B_)::value;
+    const int next_ks = ks + 1 == kb ? 0 : ks + 1;
+    i32x8 x[kFM];
+    float s[kFM];
+    x[0] = x0, s[0] = s0 * swv;
+    i32x8 xn;
+    float sn = 0.0f;
+    f32x4 p[4];  // products in flight; each is folded three products later
+    auto fold = [&](int t) __attribute__((always_inline)) {
+      const int a = t % kFN, b = t / kFN;
 #pragma unroll
-  for (int a = 0; a < kFN; ++a) {
-    const int n = n0 + wn * (BN / WN) + 16 * a + 4 * lg;
-    if (n >= N) continue;
-    const f32x4 bv = bias4(bias, n, N);
+      for (int r = 0; r < 4; ++r) acc[a][b][r] = fmaf(p[t % 4][r], s[b], acc[a][b][r]);
+    };
 #pragma unroll
     for (int b = 0; b < kFM; ++b) {
-      const int m = m0 + wm * (BM / WM) + 16 * b + li;
-      if (m < M) store4(y, m, N, n, acc[a][b] + bv);
+      if (b < kFM - 3) {
+        x[b + 1] = x_at(B, b + 1), s[b + 1] = s_at(B, b + 1) * swv;
+      } else if (b == kFM - 3) {
+#pragma unroll
+        for (int i = 1; i <= 2; ++i) x[b + i] = x_at(B, b + i), s[b + i] = s_at(B, b + i) * swv;
+      } else if (b == kFM - 2) {
+        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) and lgkmcnt(0): the next stage is here, this one is read
+        __syncthreads();
+        issue(B);
+#pragma unroll
+        for (int a = 0; a < kFN; ++a) w[1 - B][a] = w_at(1 - B, a);
+        xn = x_at(1 - B, 0), sn = s_at(1 - B, 0);
+      }
+#pragma unroll
+      for (int a = 0; a < kFN; ++a) {
+        const int t = b * kFN + a;
+        p[t % 4] = mfma128(w[B][a], x[b]);
+        if (t >= 3) fold(t - 3);
+        __builtin_amdgcn_sched_barrier(0);  // one product, one fold: the compiler would group them
+      }
     }
+#pragma unroll
+    for (int t = kFM * kFN - 3; t < kFM * kFN; ++t) fold(t);
+    x0 = xn, s0 = sn;
+    ks = next_ks;
+    if (ks == 0) {
+      store();
+      at += step;
+      if (at < end) {
+        tc = tile_at(at, tiles_m, tiles_n);
+        swp = scales();
+        clear();
+      }
+    }
+    swv = swp[ks];
+  };
+
+  aim();
+  issue(0);
+  issue(1);
+  __builtin_amdgcn_s_waitcnt(kWaitVm0);
+  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < kFN; ++a) w[0][a] = w_at(0, a);
+  x0 = x_at(0, 0), s0 = s_at(0, 0);
+  clear();
+  const std::integral_constant<int, 0> c0{};
+  const std::integral_constant<int, 1> c1{};
+  for (int i = 0; i < stages; i += 2) {
+    stage(c0);
+    if (i + 1 == stages) break;
+    stage(c1);
   }
 }
 
@@ -313,10 +412,10 @@ hipError_t launch_fp8_gemm(const uint8_t* qx, const float* sx, int64_t M, int64_
       hipLaunchKernelGGL((fp8_few_kernel<2, 2, 4>), dim3(blocks), dim3(256), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
     }
   } else if (M * N <= 256 * 256 * 256) {
-    const unsigned blocks = tiles(128, 128, &tm, &tn);
+    const unsigned blocks = std::min(tiles(128, 128, &tm, &tn), 512u);
     hipLaunchKernelGGL((fp8_gemm_kernel<128, 128, 2, 2, 2>), dim3(blocks), dim3(256), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
   } else {
-    const unsigned blocks = tiles(256, 256, &tm, &tn);
+    const unsigned blocks = std::min(tiles(256, 256, &tm, &tn), 256u);
     hipLaunchKernelGGL((fp8_gemm_kernel<256, 256, 2, 4, 2>), dim3(blocks), dim3(512), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
   }
   return hipGetLastError();
