@@ -123,10 +123,10 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
   constexpr int kWaves = WM * WN;
   constexpr int kFM = BM / WM / 16, kFN = BN / WN / 16;
   constexpr int kXDma = BM / 8 / kWaves, kWDma = BN / 8 / kWaves;  // transfers per wave and stage: 8 rows each
-  constexpr int kStage = (BM + BN) * 8;                            // 16-byte slots
+  constexpr int kXSlots = BM * 8, kWSlots = BN * 8;                // of 16 bytes, per stage
   static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && 128 % (BN / WN) == 0, "");
   static_assert(kFN == 4 && kFM >= 4 && BM / 64 <= kWaves, "");
-  __shared__ uint4 lds[2 * kStage];
+  __shared__ uint4 lds[2 * kXSlots + 2 * kWSlots];  // two stages of X, then of W: both within one offset's reach
   __shared__ float sxl[2 * BM];
 
   // XCD x takes a contiguous range of tiles, its blocks in turn.
@@ -157,32 +157,41 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
     rw = make_rsrc(qw + static_cast<int64_t>(n0) * K, min(BN, N - n0) * K);
     rs = make_rsrc(sx + static_cast<int64_t>(m0) * kb, min(BM, M - m0) * kb * 4);
   };
-  auto issue = [&](int buf) __attribute__((always_inline)) {
+  // A stage's transfers, a third at a time: a wave that issues all of them in
+  // a row stands still for them.
+  static_assert(kXDma == 4 && kWDma == 4, "");
+  constexpr bool kSpread = kFM >= 8;  // a short stage has no time to lose
+  auto issue = [&](int buf, auto part) __attribute__((always_inline)) {
     if (left == 0) return;
-    --left;
-    const uint32_t dst = lds0 + buf * kStage * 16;
     const uint32_t at = ks_to * 128 + 16 * chunk < K ? 16 * chunk + (lane >> 3) * K : kOutsideOperand;
-#pragma unroll
-    for (int j = 0; j < kXDma; ++j)
-      dma16(rx, dst + 1024 * (wave * kXDma + j), 8 * (wave * kXDma + j) * K + at, ks_to * 128);
-#pragma unroll
-    for (int j = 0; j < kWDma; ++j)
-      dma16(rw, dst + BM * 128 + 1024 * (wave * kWDma + j), 8 * (wave * kWDma + j) * K + at, ks_to * 128);
-    if (wave < BM / 64) dma4(rs, sxl0 + 4 * (buf * BM + 64 * wave), (64 * wave + lane) * kb * 4, ks_to * 4);
-    if (++ks_to == kb) {
-      ks_to = 0;
-      to += step;
-      if (left > 0) aim();
+    auto pair = [&](const Rsrc& r, uint32_t dst, int i) __attribute__((always_inline)) {
+      const int row = 8 * (4 * wave + i);
+      dma16(r, dst + 128 * row, row * K + at, ks_to * 128);
+      dma16(r, dst + 128 * row + 1024, (row + 8) * K + at, ks_to * 128);
+    };
+    const uint32_t xd = lds0 + 16 * kXSlots * buf, wd = lds0 + 16 * (2 * kXSlots + kWSlots * buf);
+    if constexpr (decltype(part)::value == 0) {
+      pair(rx, xd, 0);
+    } else if constexpr (decltype(part)::value == 1) {
+      pair(rx, xd, 2), pair(rw, wd, 0);
+    } else {
+      pair(rw, wd, 2);
+      if (wave < BM / 64) dma4(rs, sxl0 + 4 * (buf * BM + 64 * wave), (64 * wave + lane) * kb * 4, ks_to * 4);
+    }
+    if (decltype(part)::value == 2) {
+      --left;
+      if (++ks_to == kb) {
+        ks_to = 0;
+        to += step;
+        if (left > 0) aim();
+      }
     }
   };
+  const std::integral_constant<int, 0> c0{};
+  const std::integral_constant<int, 1> c1{};
+  const std::integral_constant<int, 2> c2{};
 
   f32x4 acc[kFN][kFM];
-  auto clear = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int a = 0; a < kFN; ++a)
-#pragma unroll
-      for (int b = 0; b < kFM; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
-  };
   auto frag = [&](const uint4* rows, int row) __attribute__((always_inline)) -> i32x8 {
     // lane group lg takes chunks lg and 4 + lg (any k order serves, the same on both sides)
     const int s = row & 7;
@@ -191,8 +200,8 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
     return join_regs(lo, hi);
   };
   const int xrow = wm * (BM / WM) + li, wrow = wn * (BN / WN) + li;
-  auto x_at = [&](int buf, int b) __attribute__((always_inline)) { return frag(lds + buf * kStage, xrow + 16 * b); };
-  auto w_at = [&](int buf, int a) __attribute__((always_inline)) { return frag(lds + buf * kStage + BM * 8, wrow + 16 * a); };
+  auto x_at = [&](int buf, int b) __attribute__((always_inline)) { return frag(lds + buf * kXSlots, xrow + 16 * b); };
+  auto w_at = [&](int buf, int a) __attribute__((always_inline)) { return frag(lds + 2 * kXSlots + buf * kWSlots, wrow + 16 * a); };
   auto s_at = [&](int buf, int b) __attribute__((always_inline)) { return sxl[buf * BM + xrow + 16 * b]; };
 
   // The tile being multiplied, and its weights' scales.
@@ -206,40 +215,39 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
   typedef const __attribute__((address_space(4))) float* uniform_f32;
   uniform_f32 swp = scales();
 
-  auto store = [&]() __attribute__((always_inline)) {
-    const int m0 = tc.tm * BM + xrow, n0 = tc.tn * BN + wn * (BN / WN);
+  // The sums start from the bias.
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int a = 0; a < kFN; ++a) {
+      const f32x4 v = bias4(bias, min(tc.tn * BN + wn * (BN / WN) + 16 * a + 4 * lg, N - 1), N);
+#pragma unroll
+      for (int b = 0; b < kFM; ++b) acc[a][b] = v;
+    }
+  };
+  // Row group b of the tile.
+  auto store = [&](int b) __attribute__((always_inline)) {
+    const int m = tc.tm * BM + xrow + 16 * b, n0 = tc.tn * BN + wn * (BN / WN);
     if (N % 8 == 0 && n0 + 64 <= N) {
       // Lane group lg holds columns 16 a + 4 lg ..; swapping registers between
       // groups gives it 8 consecutive ones of each 32, so that a store covers
       // 64 consecutive bytes of each of 16 rows instead of 32.
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const f32x4 b0 = bias4(bias, n0 + 32 * h + 4 * lg, N), b1 = bias4(bias, n0 + 32 * h + 16 + 4 * lg, N);
+        const f32x4 v0 = acc[2 * h][b], v1 = acc[2 * h + 1][b];
+        u32x4 out;
 #pragma unroll
-        for (int b = 0; b < kFM; ++b) {
-          const f32x4 v0 = acc[2 * h][b] + b0, v1 = acc[2 * h + 1][b] + b1;
-          u32x4 out;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const auto r = __builtin_amdgcn_permlane32_swap(pack_bf16(v0[2 * i], v0[2 * i + 1]),
-                                                            pack_bf16(v1[2 * i], v1[2 * i + 1]), false, false);
-            const auto q = __builtin_amdgcn_permlane16_swap(r[0], r[1], false, false);
-            out[i] = q[0], out[2 + i] = q[1];
-          }
-          const int m = m0 + 16 * b;
-          if (m < M) *reinterpret_cast<u32x4*>(y + static_cast<int64_t>(m) * N + n0 + 32 * h + 8 * lg) = out;
+        for (int i = 0; i < 2; ++i) {
+          const auto r = __builtin_amdgcn_permlane32_swap(pack_bf16(v0[2 * i], v0[2 * i + 1]),
+                                                          pack_bf16(v1[2 * i], v1[2 * i + 1]), false, false);
+          const auto q = __builtin_amdgcn_permlane16_swap(r[0], r[1], false, false);
+          out[i] = q[0], out[2 + i] = q[1];
         }
+        if (m < M) *reinterpret_cast<u32x4*>(y + static_cast<int64_t>(m) * N + n0 + 32 * h + 8 * lg) = out;
       }
-    } else {
+    } else if (m < M) {
 #pragma unroll
-      for (int a = 0; a < kFN; ++a) {
-        const int n = n0 + 16 * a + 4 * lg;
-        if (n >= N) continue;
-        const f32x4 bv = bias4(bias, n, N);
-#pragma unroll
-        for (int b = 0; b < kFM; ++b)
-          if (m0 + 16 * b < M) store4(y, m0 + 16 * b, N, n, acc[a][b] + bv);
-      }
+      for (int a = 0; a < kFN; ++a)
+        if (n0 + 16 * a + 4 * lg < N) store4(y, m, N, n0 + 16 * a + 4 * lg, acc[a][b]);
     }
   };
 
@@ -259,6 +267,8 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[a][b][r] = fmaf(p[t % 4][r], s[b], acc[a][b][r]);
     };
+    const bool last = next_ks == 0;  // of a tile: its row groups are stored as they are done
+    if (kSpread) issue(1 - B, c2);
 #pragma unroll
     for (int b = 0; b < kFM; ++b) {
       if (b < kFM - 3) {
@@ -269,9 +279,12 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
       } else if (b == kFM - 2) {
         __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) and lgkmcnt(0): the next stage is here, this one is read
         __syncthreads();
-        issue(B);
-#pragma unroll
-        for (int a = 0; a < kFN; ++a) w[1 - B][a] = w_at(1 - B, a);
+        issue(B, c0);
+        if (!kSpread) issue(B, c1), issue(B, c2);
+        w[1 - B][0] = w_at(1 - B, 0), w[1 - B][1] = w_at(1 - B, 1);
+      } else {
+        if (kSpread) issue(B, c1);
+        w[1 - B][2] = w_at(1 - B, 2), w[1 - B][3] = w_at(1 - B, 3);
         xn = x_at(1 - B, 0), sn = s_at(1 - B, 0);
       }
 #pragma unroll
@@ -280,14 +293,18 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
         p[t % 4] = mfma128(w[B][a], x[b]);
         if (t >= 3) fold(t - 3);
         __builtin_amdgcn_sched_barrier(0);  // one product, one fold: the compiler would group them
+        if (a == kFN - 2 && b > 0 && last) {
+          store(b - 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
 #pragma unroll
     for (int t = kFM * kFN - 3; t < kFM * kFN; ++t) fold(t);
     x0 = xn, s0 = sn;
     ks = next_ks;
-    if (ks == 0) {
-      store();
+    if (last) {
+      store(kFM - 1);
       at += step;
       if (at < end) {
         tc = tile_at(at, tiles_m, tiles_n);
@@ -299,16 +316,15 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
   };
 
   aim();
-  issue(0);
-  issue(1);
+  issue(0, c0), issue(0, c1), issue(0, c2);
+  issue(1, c0), issue(1, c1);
+  if (!kSpread) issue(1, c2);  // else at the head of the first stage
+  clear();
   __builtin_amdgcn_s_waitcnt(kWaitVm0);
   __syncthreads();
 #pragma unroll
   for (int a = 0; a < kFN; ++a) w[0][a] = w_at(0, a);
   x0 = x_at(0, 0), s0 = s_at(0, 0);
-  clear();
-  const std::integral_constant<int, 0> c0{};
-  const std::integral_constant<int, 1> c1{};
   for (int i = 0; i < stages; i += 2) {
     stage(c0);
     if (i + 1 == stages) break;
