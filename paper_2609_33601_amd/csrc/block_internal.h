@@ -34,6 +34,8 @@ hipError_t launch_pack_fp8(const uint16_t* w, int64_t N, int64_t K, uint8_t* q, 
 // y = bf16(sum over blocks of 128 k of sx * sw * (codes' product) + bias).
 hipError_t launch_fp8_gemm(const uint8_t* qx, const float* sx, int64_t M, int64_t K, const uint8_t* qw,
                            const float* sw, int64_t N, const uint16_t* bias, uint16_t* y, hipStream_t st);
+// Which of its kernels an M x K by K x N product takes on `cus` CUs.
+int fp8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t cus);
 
 struct AppendArgs {
   const uint16_t *q, *k, *v;
@@ -74,5 +76,8 @@ AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D
 hipError_t launch_paged_attention(const AttnArgs& a, hipStream_t st);
 
 }  // namespace jq
+
+// For the tests only (no part of the C ABI): the kernel that a product takes.
+extern "C" int jq_internal_fp8_route(int64_t M, int64_t N, int64_t K, int64_t cus);
 
 #endif  // JQ_BLOCK_INTERNAL_H

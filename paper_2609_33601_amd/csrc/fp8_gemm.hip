@@ -17,6 +17,7 @@
 #include "block_common.h"
 #include "block_internal.h"
 #include "gemm_common.h"
+#include "jq_internal.h"
 
 namespace jq {
 
@@ -334,16 +335,25 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
 
 // ---------------------------------------------------------------------------
 // Few output tiles.  A block takes 16 MB rows x 16 NB columns and its W waves
-// split K: wave w takes blocks of 128 k number w, w + W, ..., straight into
-// registers, no LDS or barrier in the loop.  The partial sums meet once, in
-// LDS, in wave order.
+// split K: wave w takes the blocks of 128 k number w, w + W, ...  Each wave
+// moves its operands into an LDS ring of its own, S - 1 blocks ahead, and waits
+// for nobody; the partial sums meet once, at the end, in wave order.
+// Through LDS, because eight neighbouring lanes of a transfer read one row's
+// 128 bytes: a CU takes in 123 B/ns that way.  Straight into registers,
+// neighbouring lanes are the rows of an MFMA operand, 16 bytes of each, and
+// that reaches a third of it (77 x 12288 -> 4096: 55 us).
 
-template <int MB, int NB, int W>
+template <int MB, int NB, int W, int S>
 __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
     const uint8_t* __restrict__ qx, const float* __restrict__ sx, int M, int K, const uint8_t* __restrict__ qw,
     const float* __restrict__ sw, int N, const uint16_t* __restrict__ bias, uint16_t* __restrict__ y, int tiles_m,
     int tiles_n) {
-  __shared__ f32x4 red[W * 64];
+  constexpr int kFrags = MB + NB;                   // 16 rows x 128 bytes each
+  constexpr int kOps = 2 * kFrags + 1;              // transfers of a block of k
+  constexpr int kSlots = kFrags * 128 + 16;         // 16-byte slots: the fragments, then 64 scales
+  static_assert(8 % NB == 0 && (S - 1) * kOps < 64 && MB <= 4, "");
+  constexpr int kRedSlots = W * 64 * NB;  // the sums of one row group
+  __shared__ uint4 lds[W * S * kSlots > kRedSlots ? W * S * kSlots : kRedSlots];
   TileCoord tc;
   if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, &tc)) return;
   const int m0 = 16 * MB * tc.tm, n0 = 16 * NB * tc.tn;
@@ -351,89 +361,157 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int kb = (K + 127) / 128;
-  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(qx) + static_cast<int64_t>(m0) * K, 0, min(16 * MB, M - m0) * K, kBufferFlags);
-  const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(qw) + static_cast<int64_t>(n0) * K, 0, min(16 * NB, N - n0) * K, kBufferFlags);
-  // Lane group lg takes chunks lg and 4 + lg of a row's eight (any k order
-  // serves, the same on both sides): an instruction reads 64 consecutive
-  // bytes of each of 16 rows.
-  auto load = [&](__amdgpu_buffer_rsrc_t rs, int f, int h, int ks) __attribute__((always_inline)) -> u32x4 {
-    const int at = ks * 128 + 64 * h + 16 * lg;
-    return __builtin_bit_cast(
-        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at < K ? (16 * f + li) * K + at : kOutsideOperand, 0, 0));
+  const Rsrc rx = make_rsrc(qx + static_cast<int64_t>(m0) * K, min(16 * MB, M - m0) * K);
+  const Rsrc rw = make_rsrc(qw + static_cast<int64_t>(n0) * K, min(16 * NB, N - n0) * K);
+  const Rsrc rs = make_rsrc(sx + static_cast<int64_t>(m0) * kb, min(16 * MB, M - m0) * kb * 4);
+  const uint4* ring = lds + wave * S * kSlots;
+  const uint32_t ring_at = lds_addr(ring);
+
+  // Lane l of a transfer fills slot l % 8 of row l / 8 with chunk slot ^ row, as
+  // in the kernel above.  Blocks past the last read as zeros, so that every
+  // step has the same number of transfers under way.
+  const int chunk = (lane & 7) ^ (lane >> 3);
+  const uint32_t row_at = (lane >> 3) * K + 16 * chunk;
+  auto issue = [&](int slot, int u) __attribute__((always_inline)) {
+    const uint32_t dst = ring_at + slot * kSlots * 16;
+    const bool in = u * 128 + 16 * chunk < K;
+    const uint32_t at = in ? row_at : kOutsideOperand, so = u < kb ? u * 128 : 0;
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        dma16(f < NB ? rw : rx, dst + 2048 * f + 1024 * h, at + (16 * (f < NB ? f : f - NB) + 8 * h) * K, so);
+    dma4(rs, dst + 2048 * kFrags, u < kb && lane < 16 * MB ? lane * kb * 4 + u * 4 : kOutsideOperand, 0);
   };
+  auto frag = [&](const uint4* rows) __attribute__((always_inline)) -> i32x8 {
+    const int s = li & 7;
+    return join_regs(__builtin_bit_cast(u32x4, rows[li * 8 + (lg ^ s)]),
+                     __builtin_bit_cast(u32x4, rows[li * 8 + ((4 + lg) ^ s)]));
+  };
+
   f32x4 acc[NB][MB];
 #pragma unroll
   for (int a = 0; a < NB; ++a)
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
-  for (int ks = wave; ks < kb; ks += W) {
-    i32x8 w[NB], x[MB];
-    float sxv[MB], swv[NB];
+  typedef const __attribute__((address_space(4))) float* uniform_f32;
+  const uniform_f32 swp = (uniform_f32)(sw + static_cast<int64_t>(n0 / 128) * kb);
 #pragma unroll
-    for (int a = 0; a < NB; ++a) {
-      w[a] = join_regs(load(rw, a, 0, ks), load(rw, a, 1, ks));
-      swv[a] = sw[static_cast<int64_t>(min(n0 + 16 * a, N - 1) / 128) * kb + ks];
-    }
+  for (int i = 0; i < S - 1; ++i) issue(i, wave + W * i);
+  float swv = swp[min(wave, kb - 1)];
+  int slot = 0;
+  for (int u = wave; u < kb; u += W) {
+    const float sw_next = swp[min(u + W, kb - 1)];
+    // the slot before this one has been read: it takes the block S - 1 ahead
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    issue(slot == 0 ? S - 1 : slot - 1, u + W * (S - 1));
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * kOps) : "memory");
+    const uint4* at = ring + slot * kSlots;
+    i32x8 w[NB];
+#pragma unroll
+    for (int a = 0; a < NB; ++a) w[a] = frag(at + 128 * a);
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-      x[b] = join_regs(load(rx, b, 0, ks), load(rx, b, 1, ks));
-      sxv[b] = sx[static_cast<int64_t>(min(m0 + 16 * b + li, M - 1)) * kb + ks];
-    }
+      const i32x8 x = frag(at + 128 * (NB + b));
+      const float s = reinterpret_cast<const float*>(at + 128 * kFrags)[16 * b + li] * swv;
 #pragma unroll
-    for (int a = 0; a < NB; ++a)
-#pragma unroll
-      for (int b = 0; b < MB; ++b) {
-        const f32x4 p = mfma128(w[a], x[b]);
-        const float s = sxv[b] * swv[a];
+      for (int a = 0; a < NB; ++a) {
+        const f32x4 p = mfma128(w[a], x);
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[a][b][r] = fmaf(p[r], s, acc[a][b][r]);
       }
-  }
-#pragma unroll
-  for (int a = 0; a < NB; ++a)
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-      if (a + b) __syncthreads();
-      red[wave * 64 + lane] = acc[a][b];
-      __syncthreads();
-      if (wave == 0) {
-        f32x4 v = red[lane];
-#pragma unroll
-        for (int k = 1; k < W; ++k) v += red[k * 64 + lane];
-        const int m = m0 + 16 * b + li, n = n0 + 16 * a + 4 * lg;
-        if (m < M && n < N) store4(y, m, N, n, v + bias4(bias, n, N));
-      }
     }
+    swv = sw_next;
+    slot = slot + 1 == S ? 0 : slot + 1;
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // no transfer lands in what follows
+  f32x4* red = reinterpret_cast<f32x4*>(lds);
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < NB; ++a) red[(a * W + wave) * 64 + lane] = acc[a][b];
+    __syncthreads();
+    for (int a = wave; a < NB; a += W) {
+      f32x4 v = red[a * W * 64 + lane];
+#pragma unroll
+      for (int k = 1; k < W; ++k) v += red[(a * W + k) * 64 + lane];
+      const int m = m0 + 16 * b + li, n = n0 + 16 * a + 4 * lg;
+      if (m < M && n < N) store4(y, m, N, n, v + bias4(bias, n, N));
+    }
+  }
 }
 
 }  // namespace
 
+namespace {
+
+// The kernels that a product may take, with what estimates their time in ns:
+// a launch, each round of resident blocks, and each block of 128 k that a
+// wave walks, once per round and once per block that the busiest CU has.
+// Fitted to 150 shapes (M 1 .. 2048, K 256 .. 16384, N 64 .. 16384, over their
+// logarithms) to 6 to 10% each, the tiled kernels to 17%; the kernel with the
+// lowest estimate was 1% slower than the best one on average, 19% at worst.
+// 77 x 12288 -> 4096 takes 17 us with 48 x 32 blocks and 55 us with 16 x 16
+// ones; 1 x 12288 -> 4096 takes 10 us with 16 x 16 blocks and 45 with 64 x 64.
+struct Fp8Kernel {
+  int mb, nb, waves, per_cu;            // of 16 rows and columns; waves that split K; blocks on a CU
+  float launch, round, round_k, each_k;
+};
+constexpr int kFp8Few = 8;  // those of fp8_few_kernel come first, then the two of fp8_gemm_kernel
+constexpr Fp8Kernel kFp8Kernels[kFp8Few + 2] = {
+    {1, 1, 4, 3, 1597, 999, 89, 181},  {1, 1, 8, 2, 1798, 776, 0, 393},   {1, 2, 4, 3, 1794, 734, 76, 287},
+    {2, 2, 4, 2, 1659, 1025, 32, 426}, {3, 2, 4, 1, 1128, 1632, 619, 0},  {2, 4, 4, 1, 995, 1844, 727, 0},
+    {3, 4, 2, 2, 105, 3447, 594, 131}, {4, 4, 4, 1, 311, 3020, 1105, 0},  {8, 8, 1, 2, 0, 3313, 0, 730},
+    {16, 16, 1, 1, 0, 4823, 1623, 0},
+};
+
+}  // namespace
+
+int fp8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t cus) {
+  const int64_t kb = (K + 127) / 128;
+  int best = -1;
+  float best_ns = 0;
+  for (int i = 0; i < kFp8Few + 2; ++i) {
+    const Fp8Kernel& k = kFp8Kernels[i];
+    const int64_t tiles = (M + 16 * k.mb - 1) / (16 * k.mb) * ((N + 16 * k.nb - 1) / (16 * k.nb));
+    const int64_t each = (tiles + cus - 1) / cus, rounds = (each + k.per_cu - 1) / k.per_cu;
+    const int64_t steps = (kb + k.waves - 1) / k.waves;
+    if (tiles >= (1 << 22) && i < kFp8Few) continue;  // a grid holds fewer than 2^32 threads
+    const float ns = k.launch + rounds * k.round + static_cast<float>(steps) * (rounds * k.round_k + each * k.each_k);
+    if (best < 0 || ns < best_ns) best = i, best_ns = ns;
+  }
+  return best;
+}
+
 hipError_t launch_fp8_gemm(const uint8_t* qx, const float* sx, int64_t M, int64_t K, const uint8_t* qw,
                            const float* sw, int64_t N, const uint16_t* bias, uint16_t* y, hipStream_t st) {
-  const int Mi = static_cast<int>(M), Ki = static_cast<int>(K), Ni = static_cast<int>(N);
-  auto tiles = [&](int bm, int bn, int* tm, int* tn) {
-    *tm = static_cast<int>((M + bm - 1) / bm);
-    *tn = static_cast<int>((N + bn - 1) / bn);
-    return static_cast<unsigned>((static_cast<int64_t>(*tm) * *tn + kNumXcd - 1) / kNumXcd * kNumXcd);
-  };
-  int tm, tn;
-  if (M <= 128) {
-    if (M <= 16) {
-      const unsigned blocks = tiles(16, 16, &tm, &tn);
-      hipLaunchKernelGGL((fp8_few_kernel<1, 1, 8>), dim3(blocks), dim3(512), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
-    } else {
-      const unsigned blocks = tiles(32, 32, &tm, &tn);
-      hipLaunchKernelGGL((fp8_few_kernel<2, 2, 4>), dim3(blocks), dim3(256), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
-    }
-  } else if (M * N <= 256 * 256 * 256) {
-    const unsigned blocks = std::min(tiles(128, 128, &tm, &tn), 512u);
-    hipLaunchKernelGGL((fp8_gemm_kernel<128, 128, 2, 2, 2>), dim3(blocks), dim3(256), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
-  } else {
-    const unsigned blocks = std::min(tiles(256, 256, &tm, &tn), 256u);
-    hipLaunchKernelGGL((fp8_gemm_kernel<256, 256, 2, 4, 2>), dim3(blocks), dim3(512), 0, st, qx, sx, Mi, Ki, qw, sw, Ni, bias, y, tm, tn);
+  int64_t cus;
+  const hipError_t e = device_route_cus(&cus);
+  if (e != hipSuccess) return e;
+  const int r = fp8_gemm_route(M, N, K, cus);
+  const int tm = static_cast<int>((M + 16 * kFp8Kernels[r].mb - 1) / (16 * kFp8Kernels[r].mb));
+  const int tn = static_cast<int>((N + 16 * kFp8Kernels[r].nb - 1) / (16 * kFp8Kernels[r].nb));
+  const int64_t tiles = (static_cast<int64_t>(tm) * tn + kNumXcd - 1) / kNumXcd * kNumXcd;
+#define JQ_FP8(KERNEL, BLOCKS, THREADS)                                                                          \
+  hipLaunchKernelGGL((KERNEL), dim3(static_cast<unsigned>(BLOCKS)), dim3(THREADS), 0, st, qx, sx,                \
+                     static_cast<int>(M), static_cast<int>(K), qw, sw, static_cast<int>(N), bias, y, tm, tn)
+#define JQ_FEW(MB, NB, W, S) JQ_FP8((fp8_few_kernel<MB, NB, W, S>), tiles, 64 * W)
+  switch (r) {
+    case 0: JQ_FEW(1, 1, 4, 3); break;
+    case 1: JQ_FEW(1, 1, 8, 2); break;
+    case 2: JQ_FEW(1, 2, 4, 2); break;
+    case 3: JQ_FEW(2, 2, 4, 2); break;
+    case 4: JQ_FEW(3, 2, 4, 2); break;
+    case 5: JQ_FEW(2, 4, 4, 2); break;
+    case 6: JQ_FEW(3, 4, 2, 2); break;
+    case 7: JQ_FEW(4, 4, 4, 2); break;
+    // these walk tiles of their own accord: as many blocks as fit the device
+    case 8: JQ_FP8((fp8_gemm_kernel<128, 128, 2, 2, 2>), std::min(tiles, 2 * cus), 256); break;
+    default: JQ_FP8((fp8_gemm_kernel<256, 256, 2, 4, 2>), std::min(tiles, cus), 512); break;
   }
+#undef JQ_FEW
+#undef JQ_FP8
   return hipGetLastError();
 }
 

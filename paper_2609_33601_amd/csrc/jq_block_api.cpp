@@ -166,6 +166,8 @@ jq_status jq_fp8_gemm(const void* q, const float* scale, int64_t M, int64_t K, c
                                       w_scale, N, u16(bias_bf16), static_cast<uint16_t*>(y_bf16), as_stream(stream)));
 }
 
+int jq_internal_fp8_route(int64_t M, int64_t N, int64_t K, int64_t cus) { return jq::fp8_gemm_route(M, N, K, cus); }
+
 jq_status jq_fp8_linear(const void* x_bf16, int64_t x_stride, int64_t M, int64_t K, const void* wq,
                         const float* w_scale, int64_t N, const void* bias_bf16, void* y_bf16, void* workspace,
                         size_t workspace_bytes, void* stream) {

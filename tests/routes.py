@@ -27,6 +27,13 @@ def route(kind, M, K, N, G=0, cus=256):
     return Route(KERNELS[out[0]], out[1], out[2], out[3])
 
 
+def fp8_route(M, K, N, cus=256):
+    """The kernel, 0 to 9, of an 8-bit M x K by K x N product."""
+    fn = jq.lib().jq_internal_fp8_route
+    fn.argtypes, fn.restype = [ctypes.c_int64] * 4, ctypes.c_int
+    return fn(M, N, K, cus)
+
+
 def few_rows(M, K, G=0):
     """Whether the BF6 quantiser takes the few-row kernel for an M x K input."""
     fn = jq.lib().jq_internal_quantize_few

@@ -149,6 +149,18 @@ def test_attention_workspace():
     assert _call("jq_paged_attention", ATTEND, ws=A + 64, n=need, **long) == ALIGN
 
 
+def test_gemm_routes():
+    """The GPU tests' products run on every kernel, and every size has one."""
+    from tests.routes import fp8_route
+    from tests.test_gpu_block import GEMM_SHAPES
+
+    assert {fp8_route(*s) for s in GEMM_SHAPES} == set(range(10))
+    # many small blocks would not fit a grid: the tiled kernels take those
+    for M, K, N in ((1 << 30, 16, 1), (1 << 25, 16, 1 << 12), (1 << 16, 65536, 1 << 22)):
+        assert fp8_route(M, K, N) in (8, 9)
+    assert fp8_route(1, 65536, 1 << 22) in range(10)
+
+
 def test_binding_refuses():
     torch = pytest.importorskip("torch")
     x = torch.zeros((4, 64), dtype=torch.bfloat16)
