@@ -37,7 +37,8 @@ ARCH = "gfx950"
 SOURCE_FLAGS = {"f6.hip": ["-mllvm", "-disable-machine-sink"], "fp8_gemm.hip": ["-mllvm", "-disable-machine-sink"]}
 # Sources whose asm-issued loads are checked against their waits, and the
 # kernel names checked in each.
-CHECKED_SOURCES = {"f6.hip": "w4a4_f6_gemm_kernel", "fp8_gemm.hip": "fp8_gemm_kernel"}
+CHECKED_SOURCES = {"f6.hip": "w4a4_f6_gemm_kernel", "fp8_gemm.hip": "fp8_gemm_kernel",
+                   "paged_attention.hip": "paged_attention_wide_kernel"}
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}",

@@ -115,6 +115,38 @@ __device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
               umax(static_cast<uint32_t>(__builtin_amdgcn_readlane(i, 32)), static_cast<uint32_t>(__builtin_amdgcn_readlane(i, 48))));
 }
 
+// Transfers from a buffer into LDS, 16 (or 4) bytes per lane: lane i writes
+// lds + 16 i (4 i).  As asm, because the compiler waits for transfers that it
+// knows of before the next LDS read, whatever part of LDS that reads, and the
+// whole point of several stages is not to.  A kernel waits itself (vmcnt).  The
+// wait states that the compiler would put behind the writes of M0 and of
+// descriptor words are in the asm; the build checks them.
+constexpr int kRawBuffer = 0x00020000;             // descriptor word 3: raw bytes
+constexpr uint32_t kOutsideBuffer = 0x80000000u;   // an offset past every descriptor here: reads as zero
+struct Rsrc {
+  u32x4 w;
+};
+__device__ __forceinline__ Rsrc make_rsrc(const void* base, int bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32)) & 0xFFFFu;
+  const uint32_t n = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(bytes));
+  return {u32x4{lo, hi, n, static_cast<uint32_t>(kRawBuffer)}};
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
+}
+__device__ __forceinline__ void dma16(const Rsrc& r, uint32_t lds, uint32_t voffset, uint32_t soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voffset), "s"(r.w), "s"(soffset)
+               : "memory");
+}
+__device__ __forceinline__ void dma4(const Rsrc& r, uint32_t lds, uint32_t voffset, uint32_t soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voffset), "s"(r.w), "s"(soffset)
+               : "memory");
+}
+
 }  // namespace block_detail
 }  // namespace jq
 

@@ -24,9 +24,7 @@ namespace jq {
 namespace {
 
 using namespace block_detail;
-using gemm_detail::kBufferFlags;
 using gemm_detail::kNumXcd;
-using gemm_detail::kOutsideOperand;
 using gemm_detail::kWaitVm0;
 using gemm_detail::tile_of_block;
 using gemm_detail::TileCoord;
@@ -41,37 +39,6 @@ __device__ __forceinline__ i32x8 join_regs(u32x4 a, u32x4 b) {
 // One block of 128 k: W rows x X rows from zero.
 __device__ __forceinline__ f32x4 mfma128(i32x8 w, i32x8 x) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-}
-
-// Transfers from a buffer into LDS, 16 (or 4) bytes per lane: lane i writes
-// lds + 16 i (4 i).  As asm, because the compiler waits for transfers that it
-// knows of before the next LDS read, whatever part of LDS that reads, and the
-// whole point of two stages is not to.  The kernel waits itself (vmcnt(0) at
-// the head of a stage).  The wait states that the compiler would put behind the
-// writes of M0 and of descriptor words are in the asm; the build checks them.
-typedef unsigned u32x4s __attribute__((ext_vector_type(4)));
-struct Rsrc {
-  u32x4s w;
-};
-__device__ __forceinline__ Rsrc make_rsrc(const void* base, int bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(base);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32)) & 0xFFFFu;
-  const uint32_t n = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(bytes));
-  return {u32x4s{lo, hi, n, static_cast<uint32_t>(kBufferFlags)}};
-}
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
-}
-__device__ __forceinline__ void dma16(const Rsrc& r, uint32_t lds, uint32_t voffset, uint32_t soffset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voffset), "s"(r.w), "s"(soffset)
-               : "memory");
-}
-__device__ __forceinline__ void dma4(const Rsrc& r, uint32_t lds, uint32_t voffset, uint32_t soffset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
-               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voffset), "s"(r.w), "s"(soffset)
-               : "memory");
 }
 
 // Tile t in the grouped order of tile_of_block: 8 tiles of m per sweep of n.
@@ -164,7 +131,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
   constexpr bool kSpread = kFM >= 8;  // a short stage has no time to lose
   auto issue = [&](int buf, auto part) __attribute__((always_inline)) {
     if (left == 0) return;
-    const uint32_t at = ks_to * 128 + 16 * chunk < K ? 16 * chunk + (lane >> 3) * K : kOutsideOperand;
+    const uint32_t at = ks_to * 128 + 16 * chunk < K ? 16 * chunk + (lane >> 3) * K : kOutsideBuffer;
     auto pair = [&](const Rsrc& r, uint32_t dst, int i) __attribute__((always_inline)) {
       const int row = 8 * (4 * wave + i);
       dma16(r, dst + 128 * row, row * K + at, ks_to * 128);
@@ -375,13 +342,13 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
   auto issue = [&](int slot, int u) __attribute__((always_inline)) {
     const uint32_t dst = ring_at + slot * kSlots * 16;
     const bool in = u * 128 + 16 * chunk < K;
-    const uint32_t at = in ? row_at : kOutsideOperand, so = u < kb ? u * 128 : 0;
+    const uint32_t at = in ? row_at : kOutsideBuffer, so = u < kb ? u * 128 : 0;
 #pragma unroll
     for (int f = 0; f < kFrags; ++f)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         dma16(f < NB ? rw : rx, dst + 2048 * f + 1024 * h, at + (16 * (f < NB ? f : f - NB) + 8 * h) * K, so);
-    dma4(rs, dst + 2048 * kFrags, u < kb && lane < 16 * MB ? lane * kb * 4 + u * 4 : kOutsideOperand, 0);
+    dma4(rs, dst + 2048 * kFrags, u < kb && lane < 16 * MB ? lane * kb * 4 + u * 4 : kOutsideBuffer, 0);
   };
   auto frag = [&](const uint4* rows) __attribute__((always_inline)) -> i32x8 {
     const int s = li & 7;

@@ -28,7 +28,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <stdlib.h>
 #include <algorithm>
+#include <type_traits>
 
 #include "block_common.h"
 #include "block_internal.h"
@@ -41,6 +43,7 @@ using namespace block_detail;
 
 constexpr int kWaves = 4;
 constexpr int kTile = 32;  // tokens of a wave's step
+typedef const __attribute__((address_space(4))) int32_t* uniform_i32;
 constexpr float kNegInf = -__builtin_inff();
 
 // Largest over the lanes that differ in the upper two lane bits.
@@ -85,328 +88,572 @@ struct PartView {
 };
 __host__ __device__ __forceinline__ PartView part_view(float* ws, int64_t rows, int D) { return {ws, ws + rows * D}; }
 
-// NG groups of 16 columns per wave.
-template <int D, bool FP8, int NG, int WPS>
-__global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const AttnArgs a, int chunk, int parts,
-                                                                           int col_blocks) {
+// Where a block is: heads run fastest, so that with the usual numbers of heads
+// an XCD (every eighth block) has its share of every sequence, however their
+// lengths differ, and blocks with the same keys share its cache; the last
+// parts, which most sequences do not have, come last.
+struct BlockPlace {
+  int hk, b, cb, part;
+};
+__device__ __forceinline__ BlockPlace block_place(const AttnArgs& a, int col_blocks) {
+  const int id = blockIdx.x, bh = id / a.Hk;
+  return {id % a.Hk, bh % a.B, bh / a.B % col_blocks, bh / a.B / col_blocks};
+}
+
+// The queries of column `col` (new token, head of the key head's group): the
+// new token, the row in [B, Tq, Hq] and the operand of the first product.
+template <int D, bool FP8>
+struct Query {
+  int token;
+  int64_t row;
+  bf16x8 f[D / 32];
+  __device__ __forceinline__ void load(const AttnArgs& a, int b, int hk, int col, int lg) {
+    const int G = a.Hq / a.Hk;
+    token = col / G;
+    row = (static_cast<int64_t>(b) * a.Tq + token) * a.Hq + hk * G + (col - token * G);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      // which eight of a head a lane feeds to step c: with bytes, sixteen consecutive values serve two steps
+      const int d = FP8 ? 64 * (c / 2) + 16 * lg + 8 * (c % 2) : 32 * c + 8 * lg;
+      f[c] = *reinterpret_cast<const bf16x8*>(a.q + row * D + d);
+    }
+  }
+};
+
+// S^T of 16 tokens: their rows' 16-byte chunks 4 c + lg, times the queries.
+template <int D, bool FP8>
+__device__ __forceinline__ f32x4 scores(const uint32_t* k, const Query<D, FP8>& q) {
+  f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    u32x4 kv;
+    if constexpr (FP8) {
+      const uint32_t w0 = k[2 * c], w1 = k[2 * c + 1];
+      kv = u32x4{e4m3_pair_to_bf16<false>(w0), e4m3_pair_to_bf16<true>(w0), e4m3_pair_to_bf16<false>(w1),
+                 e4m3_pair_to_bf16<true>(w1)};
+    } else {
+      kv = u32x4{k[4 * c], k[4 * c + 1], k[4 * c + 2], k[4 * c + 3]};
+    }
+    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kv), q.f[c], s, 0, 0, 0);
+  }
+  return s;
+}
+
+// N more scores of a lane's column (in powers of two; -inf: not seen): their
+// powers, with the running maximum, sum and output brought along.
+template <int N, int DV>
+__device__ __forceinline__ void online_softmax(float (&v)[N], float& m, float& l, f32x4 (&o)[DV]) {
+  float top = v[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
+  top = fmaxf(max_groups(top), m);
+  const float base = top == kNegInf ? 0.0f : top;  // nothing seen yet: every power below is 0
+  if (__any(top != m)) {
+    const float keep = __builtin_amdgcn_exp2f(m - base);
+    l *= keep;
+#pragma unroll
+    for (int j = 0; j < DV; ++j) o[j] *= keep;
+    m = top;
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    v[e] = __builtin_amdgcn_exp2f(v[e] - base);
+    l += v[e];
+  }
+}
+
+// O^T += V^T P^T of 32 tokens, one MFMA per value of a lane's V rows: v[e] are
+// D / 16 consecutive values of tokens 4 lg + e % 4 of both groups of 16.
+template <int D, bool FP8, int ROW>
+__device__ __forceinline__ void add_values(const uint32_t (*v)[ROW], bf16x8 p, f32x4 (&o)[D / 16]) {
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) {
+    u32x4 r;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      uint32_t x, y;  // the dwords of tokens 2h and 2h + 1 that hold value j
+      if constexpr (FP8) {
+        const uint32_t wx = v[2 * h][j / 4], wy = v[2 * h + 1][j / 4];
+        x = (j & 2) ? e4m3_pair_to_bf16<true>(wx) : e4m3_pair_to_bf16<false>(wx);
+        y = (j & 2) ? e4m3_pair_to_bf16<true>(wy) : e4m3_pair_to_bf16<false>(wy);
+      } else {
+        x = v[2 * h][j / 2];
+        y = v[2 * h + 1][j / 2];
+      }
+      r[h] = __builtin_amdgcn_perm(y, x, (j & 1) ? 0x07060302u : 0x05040100u);
+    }
+    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), p, o[j], 0, 0, 0);
+  }
+}
+
+__device__ __forceinline__ float log_sum(float top, float sum) {
+  return sum == 0.0f ? kNegInf : (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
+}
+
+// Up to 16 columns: the waves of a block take steps of 32 tokens in turn.
+template <int D, bool FP8, int WPS>
+__global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const AttnArgs a, int chunk, int parts) {
   constexpr int kB = FP8 ? 1 : 2;   // bytes of a cached value
   constexpr int kDV = D / 16;       // values of a V row per lane
-  constexpr int kKS = D / 32;       // k-steps of the first product
+  constexpr int kVRow = kDV * kB / 4;
   __shared__ float red_o[kWaves * 16 * (D + 4)];
   __shared__ float red_m[kWaves * 16], red_l[kWaves * 16];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
-  // Blocks that share a part's keys lie next to each other; parts of one head follow.
-  int id = blockIdx.x;
-  const int cb = id % col_blocks;
-  id /= col_blocks;
-  const int part = id % parts;
-  id /= parts;
-  const int hk = id % a.Hk;
-  const int b = id / a.Hk;
-
-  const int G = a.Hq / a.Hk;
-  const int cols = a.Tq * G;
+  const BlockPlace at = block_place(a, 1);
+  const int b = at.b, hk = at.hk, part = at.part;
+  const int G = a.Hq / a.Hk, cols = a.Tq * G;
   const int page = 1 << a.page_shift;
-  int len = a.lens[b];
-  len = min(len, a.max_len);
-  const int t0 = part * chunk;
-  const int t1 = min(len, t0 + chunk);
+  const int len = min(a.lens[b], a.max_len);
+  const int t0 = part * chunk, t1 = min(len, t0 + chunk);
   const bool direct = parts == 1;
   if (t0 >= t1 && !direct) return;  // the joining kernel counts parts by len, too
 
-  // Queries: column -> (new token, head of the group).  Columns past the last repeat it.
-  int qi[NG];        // new token of this lane's column
-  int64_t qrow[NG];  // its row in [B, Tq, Hq]
-  bf16x8 qf[NG][kKS];
-#pragma unroll
-  for (int n = 0; n < NG; ++n) {
-    const int col = min((cb * NG + n) * 16 + li, cols - 1);
-    qi[n] = col / G;
-    qrow[n] = (static_cast<int64_t>(b) * a.Tq + qi[n]) * a.Hq + hk * G + (col - qi[n] * G);
-    const uint16_t* qp = a.q + qrow[n] * D;
-#pragma unroll
-    for (int c = 0; c < kKS; ++c) {
-      // which eight of a head a lane feeds to step c: with bytes, sixteen consecutive values serve two steps
-      const int d = FP8 ? 64 * (c / 2) + 16 * lg + 8 * (c % 2) : 32 * c + 8 * lg;
-      qf[n][c] = *reinterpret_cast<const bf16x8*>(qp + d);
-    }
-  }
+  Query<D, FP8> q;
+  q.load(a, b, hk, min(li, cols - 1), lg);  // columns past the last repeat it
+  const int end = a.causal ? min(len, len - a.Tq + 1 + q.token) : len;
 
-  f32x4 o[NG][kDV];
-  float m[NG], l[NG];
+  f32x4 o[kDV];
 #pragma unroll
-  for (int n = 0; n < NG; ++n) {
-    m[n] = kNegInf, l[n] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < kDV; ++j) o[n][j] = f32x4{0, 0, 0, 0};
-  }
+  for (int j = 0; j < kDV; ++j) o[j] = f32x4{0, 0, 0, 0};
+  float m = kNegInf, l = 0.0f;
   const float scale2 = a.scale * 1.44269504088896340736f;  // exponentials are powers of two
-  const int32_t* table = a.table + static_cast<int64_t>(b) * a.table_cols;
+  // read with scalar loads: uniform, and nobody writes it meanwhile
+  const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   const uint8_t* kbase = static_cast<const uint8_t*>(a.k_cache);
   const uint8_t* vbase = static_cast<const uint8_t*>(a.v_cache);
   bool bad = false;  // a page number outside the cache was met
 
-  for (int tile = t0 + wave * kTile; tile < t1; tile += kWaves * kTile) {
-    // Pages hold 16 tokens or more, so each half of a tile lies in one page.
-    // Tokens past the end read the last one (finite numbers that count for nothing).
-    int64_t line[2];  // first cached row of the half
-    int last[2];      // its last readable place
+  // A step's place: the first cached row of each group of 16 tokens, and the
+  // group's last readable one.  Pages hold 16 tokens or more, so a group lies in
+  // one page.  Tokens past the end read the last one of their group, groups past
+  // the end the first group.
+  struct Place {
+    int64_t line[2];
+    int last[2];
+  };
+  auto locate = [&](int tile) __attribute__((always_inline)) -> Place {
+    Place p;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int h0 = tile + 16 * s < len ? tile + 16 * s : tile;
-      const int pi = h0 >> a.page_shift;
-      int pg = table[pi];
+      int pg = table[h0 >> a.page_shift];
       if (pg < 0 || pg >= a.num_pages) bad = true, pg = 0;
-      line[s] = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
-      last[s] = min(len - 1 - h0, 15);
+      p.line[s] = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
+      p.last[s] = min(len - 1 - h0, 15);
     }
-
-    uint32_t kf[2][kKS * 4 * kB / 2];
-    float ks[2][4], vs[2][4];
+    return p;
+  };
+  uint32_t kf[2][D * kB / 16], vf[8][kVRow];
+  float ks[2][4], vs[2][4];
+  auto load_k = [&](const Place& p) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const uint8_t* kp = kbase + (line[s] + min(li, last[s])) * (D * kB);
+      const uint8_t* kp = kbase + (p.line[s] + min(li, p.last[s])) * (D * kB) + 16 * lg;
 #pragma unroll
-      for (int c = 0; c < kKS * kB / 2; ++c) load_bytes<16>(kp + 64 * c + 16 * lg, kf[s] + 4 * c);
-      if constexpr (FP8) {
-        *reinterpret_cast<f32x4*>(ks[s]) = *reinterpret_cast<const f32x4*>(a.k_scale + line[s] + 4 * lg);
-        *reinterpret_cast<f32x4*>(vs[s]) = *reinterpret_cast<const f32x4*>(a.v_scale + line[s] + 4 * lg);
+      for (int c = 0; c < D * kB / 64; ++c) load_bytes<16>(kp + 64 * c, kf[s] + 4 * c);
+      if constexpr (FP8) *reinterpret_cast<f32x4*>(ks[s]) = *reinterpret_cast<const f32x4*>(a.k_scale + p.line[s] + 4 * lg);
+    }
+  };
+  auto load_v = [&](const Place& p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if constexpr (FP8) *reinterpret_cast<f32x4*>(vs[s]) = *reinterpret_cast<const f32x4*>(a.v_scale + p.line[s] + 4 * lg);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        load_bytes<kDV * kB>(vbase + (p.line[s] + min(4 * lg + e, p.last[s])) * (D * kB) + li * (kDV * kB), vf[4 * s + e]);
+    }
+  };
+
+  // The next step's keys are requested when this one's have been multiplied,
+  // and its values when this one's have: the registers are free by then, and
+  // a wave always has a step on its way.
+  auto step = [&](int tile, auto more) __attribute__((always_inline)) {
+    Place next;
+    if constexpr (more) next = locate(tile + kWaves * kTile);
+
+    // this lane's column, tokens tile + 16 s + 4 lg + r
+    float v[8];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const f32x4 sc = scores<D, FP8>(kf[s], q);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = sc[r] * scale2;
+        if constexpr (FP8) x *= ks[s][r];
+        v[4 * s + r] = tile + 16 * s + 4 * lg + r < end ? x : kNegInf;
       }
     }
-    uint32_t vf[8][kDV * kB / 4];
+    if constexpr (more) load_k(next);
+    bool seen[8];
+    if constexpr (FP8) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int s = e / 4;
-      const uint8_t* vp = vbase + (line[s] + min(4 * lg + e % 4, last[s])) * (D * kB);
-      load_bytes<kDV * kB>(vp + li * (kDV * kB), vf[e]);
+      for (int e = 0; e < 8; ++e) seen[e] = !(v[e] == kNegInf);
     }
-
-    // scores
-    f32x4 sc[NG][2];
+    online_softmax(v, m, l, o);
+    if constexpr (FP8) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int c = 0; c < kKS; ++c) {
-        bf16x8 kv;
-        if constexpr (FP8) {
-          const uint32_t w0 = kf[s][2 * c], w1 = kf[s][2 * c + 1];
-          kv = __builtin_bit_cast(bf16x8, u32x4{e4m3_pair_to_bf16<false>(w0), e4m3_pair_to_bf16<true>(w0),
-                                                e4m3_pair_to_bf16<false>(w1), e4m3_pair_to_bf16<true>(w1)});
-        } else {
-          kv = __builtin_bit_cast(bf16x8, u32x4{kf[s][4 * c], kf[s][4 * c + 1], kf[s][4 * c + 2], kf[s][4 * c + 3]});
-        }
-#pragma unroll
-        for (int n = 0; n < NG; ++n)
-          sc[n][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qf[n][c], c ? sc[n][s] : f32x4{0, 0, 0, 0}, 0, 0, 0);
-      }
-
-    // softmax: this lane's column, tokens tile + 16 s + 4 lg + r
-    bf16x8 p[NG];
-#pragma unroll
-    for (int n = 0; n < NG; ++n) {
-      const int end = a.causal ? min(len, len - a.Tq + 1 + qi[n]) : len;
-      float v[8];
-      float top = kNegInf;
+      for (int e = 0; e < 8; ++e) v[e] = seen[e] ? v[e] * vs[e / 4][e % 4] : 0.0f;
+    }
+    // Only a wave's last step may reach past the end.  The rows read there count
+    // for nothing, which an infinity times 0 would not do.
+    if constexpr (!more) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int t = tile + 16 * (e / 4) + 4 * lg + e % 4;
-        float x = sc[n][e / 4][e % 4] * scale2;
-        if constexpr (FP8) x *= ks[e / 4][e % 4];
-        v[e] = t < end ? x : kNegInf;
-        top = fmaxf(top, v[e]);
-      }
-      top = fmaxf(max_groups(top), m[n]);
-      const float base = top == kNegInf ? 0.0f : top;  // nothing seen yet: every power below is 0
-      if (__any(top != m[n])) {
-        const float keep = __builtin_amdgcn_exp2f(m[n] - base);
-        l[n] *= keep;
+        const bool in = tile + 16 * (e / 4) + 4 * lg + e % 4 < len;
 #pragma unroll
-        for (int j = 0; j < kDV; ++j) o[n][j] *= keep;
-        m[n] = top;
+        for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
-      float pe[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        pe[e] = __builtin_amdgcn_exp2f(v[e] - base);
-        l[n] += pe[e];
-        if constexpr (FP8) pe[e] = v[e] == kNegInf ? 0.0f : pe[e] * vs[e / 4][e % 4];
-      }
-      p[n] = __builtin_bit_cast(bf16x8, pack8_bf16(pe));
     }
-
-    // O^T += V^T P^T, one MFMA per value of a lane's V rows
-    auto vt = [&](int j) __attribute__((always_inline)) -> bf16x8 {
-      u32x4 r;
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        uint32_t x, y;  // the dwords of tokens 2h and 2h + 1 that hold value j
-        if constexpr (FP8) {
-          const uint32_t wx = vf[2 * h][j / 4], wy = vf[2 * h + 1][j / 4];
-          x = (j & 2) ? e4m3_pair_to_bf16<true>(wx) : e4m3_pair_to_bf16<false>(wx);
-          y = (j & 2) ? e4m3_pair_to_bf16<true>(wy) : e4m3_pair_to_bf16<false>(wy);
-        } else {
-          x = vf[2 * h][j / 2];
-          y = vf[2 * h + 1][j / 2];
-        }
-        r[h] = __builtin_amdgcn_perm(y, x, (j & 1) ? 0x07060302u : 0x05040100u);
-      }
-      return __builtin_bit_cast(bf16x8, r);
-    };
-#pragma unroll
-    for (int j = 0; j < kDV; ++j) {
-      const bf16x8 v = vt(j);
-#pragma unroll
-      for (int n = 0; n < NG; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[n], o[n][j], 0, 0, 0);
-    }
+    add_values<D, FP8>(vf, __builtin_bit_cast(bf16x8, pack8_bf16(v)), o);
+    if constexpr (more) load_v(next);
+  };
+  int tile = t0 + wave * kTile;
+  if (tile < t1) {
+    const Place first = locate(tile);
+    load_k(first);
+    load_v(first);
+    for (; tile + kWaves * kTile < t1; tile += kWaves * kTile) step(tile, std::true_type{});
+    step(tile, std::false_type{});
   }
-
-  if (__any(bad)) {
-#pragma unroll
-    for (int n = 0; n < NG; ++n) l[n] = __builtin_nanf(""), m[n] = 0.0f;
-  }
+  if (__any(bad)) l = __builtin_nanf(""), m = 0.0f;
 
   // Join the waves.  A lane holds, of column li, values d = kDV (4 lg + r) + j:
-  // kDV * 4 in a row, from kDV * 4 * lg.
-  const PartView pv = part_view(a.ws, static_cast<int64_t>(a.B) * a.Hk * parts * cols, D);
+  // 4 kDV in a row, from 4 kDV lg.
+  l = sum_groups(l);
+  float* mine = red_o + (wave * 16 + li) * (D + 4) + kDV * 4 * lg;
 #pragma unroll
-  for (int n = 0; n < NG; ++n) {
-    if (n) __syncthreads();
-    const float ln = sum_groups(l[n]);
-    float* mine = red_o + (wave * 16 + li) * (D + 4) + kDV * 4 * lg;
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int j = 0; j < kDV; j += 4)
+      *reinterpret_cast<f32x4*>(mine + r * kDV + j) = f32x4{o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]};
+  if (lg == 0) red_m[wave * 16 + li] = m, red_l[wave * 16 + li] = l;
+  __syncthreads();
+  // thread -> (column, D / 16 values)
+  const int c = threadIdx.x / 16, d0 = (threadIdx.x % 16) * kDV;
+  if (c >= cols) return;
+  float top = red_m[c];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w * 16 + c]);
+  const float base = top == kNegInf ? 0.0f : top;
+  float sum = 0.0f, acc[kDV];
+#pragma unroll
+  for (int j = 0; j < kDV; ++j) acc[j] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float f = __builtin_amdgcn_exp2f(red_m[w * 16 + c] - base);
+    sum += f * red_l[w * 16 + c];
+#pragma unroll
+    for (int j = 0; j < kDV; ++j) acc[j] += f * red_o[(w * 16 + c) * (D + 4) + d0 + j];
+  }
+  if (direct) {
+    const int tq = c / G;
+    const int64_t row = (static_cast<int64_t>(b) * a.Tq + tq) * a.Hq + hk * G + (c - tq * G);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D + d0);
+#pragma unroll
+    for (int j = 0; j < kDV / 2; ++j) dst[j] = pack_bf16(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+    if (a.lse != nullptr && d0 == 0) a.lse[row] = log_sum(top, sum);
+  } else {
+    const PartView pv = part_view(a.ws, static_cast<int64_t>(a.B) * a.Hk * parts * cols, D);
+    const int64_t row = ((static_cast<int64_t>(b) * a.Hk + hk) * parts + part) * cols + c;
+#pragma unroll
+    for (int j = 0; j < kDV; j += 4)
+      *reinterpret_cast<f32x4*>(pv.o + row * D + d0 + j) = f32x4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
+    if (d0 == 0) *reinterpret_cast<float2*>(pv.ml + 2 * row) = make_float2(top, sum);
+  }
+}
+
+// More columns: a block takes 64 of them, 16 a wave, and all its waves the same
+// 64 tokens at a time, which transfers bring into LDS once for all of them,
+// each wave a group of 16, one stage ahead of the products.  A row's 16-byte
+// chunk c sits at chunk c ^ (row & 15) of its place in LDS (as far as the row
+// has chunks), so that the sixteen rows an operand spans cover all banks.
+template <int D, bool FP8, int WPS>
+__global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_wide_kernel(const AttnArgs a, int chunk, int parts,
+                                                                                int col_blocks) {
+  constexpr int kB = FP8 ? 1 : 2;
+  constexpr int kDV = D / 16, kVRow = kDV * kB / 4;
+  constexpr int kRow = D * kB;                     // bytes of a cached row
+  constexpr int kChunks = kRow / 16;
+  constexpr int kMask = (kChunks < 16 ? kChunks : 16) - 1;
+  constexpr int kRows = 1024 / kRow;               // rows of a transfer
+  constexpr int kGroup = 16 * kRow;                // bytes of a group of 16 tokens
+  constexpr int kKeys = kWaves * kGroup, kStage = 2 * kKeys + 512;  // keys, values, their scales
+  static_assert(kRows >= 1 && kRows <= 16, "");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStage];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, lg = lane >> 4;
+  const BlockPlace at = block_place(a, col_blocks);
+  const int b = at.b, hk = at.hk, part = at.part;
+  const int G = a.Hq / a.Hk, cols = a.Tq * G;
+  const int page = 1 << a.page_shift;
+  const int len = min(a.lens[b], a.max_len);
+  const int t0 = part * chunk, t1 = min(len, t0 + chunk);
+  const bool direct = parts == 1;
+  if (t0 >= t1 && !direct) return;
+
+  const int col0 = 64 * at.cb + 16 * wave;
+  const bool busy = col0 < cols;  // else this wave only moves data
+  Query<D, FP8> q;
+  q.load(a, b, hk, min(col0 + li, cols - 1), lg);
+  const int end = a.causal ? min(len, len - a.Tq + 1 + q.token) : len;
+  f32x4 o[kDV];
+#pragma unroll
+  for (int j = 0; j < kDV; ++j) o[j] = f32x4{0, 0, 0, 0};
+  float m = kNegInf, l = 0.0f;
+  const float scale2 = a.scale * 1.44269504088896340736f;
+  const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
+  bool bad = false;
+  const uint32_t lds0 = lds_addr(lds);
+
+  // This wave's group of a stage: 16 rows that lie in one page.  Groups past the
+  // end read the stage's first one; what lies past the end counts for nothing.
+  auto issue = [&](int buf, int tile) __attribute__((always_inline)) {
+    const int h0 = tile + 16 * wave < len ? tile + 16 * wave : tile;
+    int pg = table[h0 >> a.page_shift];
+    if (pg < 0 || pg >= a.num_pages) bad = true, pg = 0;
+    const int64_t line = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
+    const Rsrc rk = make_rsrc(static_cast<const uint8_t*>(a.k_cache) + line * kRow, kGroup);
+    const Rsrc rv = make_rsrc(static_cast<const uint8_t*>(a.v_cache) + line * kRow, kGroup);
+    const uint32_t dst = lds0 + buf * kStage + wave * kGroup;
+#pragma unroll
+    for (int i = 0; i < kGroup / 1024; ++i) {
+      const int row = kRows * i + lane / kChunks, c = lane % kChunks;
+      const uint32_t from = row * kRow + 16 * (c ^ (row & kMask));
+      dma16(rk, dst + 1024 * i, from, 0);
+      dma16(rv, dst + kKeys + 1024 * i, from, 0);
+    }
+    if constexpr (FP8) {
+      const Rsrc rks = make_rsrc(a.k_scale + line, 64), rvs = make_rsrc(a.v_scale + line, 64);
+      const uint32_t sc = lds0 + buf * kStage + 2 * kKeys;
+      if (lane < 16) {
+        dma4(rks, sc + 64 * wave, 4 * lane, 0);
+        dma4(rvs, sc + 256 + 64 * wave, 4 * lane, 0);
+      }
+    }
+  };
+
+  if (t0 < t1) issue(0, t0);
+  int buf = 0;
+  for (int tile = t0; tile < t1; tile += 64, buf ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tile + 64 < t1) issue(buf ^ 1, tile + 64);
+    if (!busy) continue;
+    const uint8_t* keys = lds + buf * kStage;
+    const uint8_t* values = keys + kKeys;
+    const float* ks = reinterpret_cast<const float*>(keys + 2 * kKeys);
+    float v[16];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      uint32_t kf[kRow / 16];
+#pragma unroll
+      for (int c = 0; c < kRow / 64; ++c)
+        load_bytes<16>(keys + s * kGroup + li * kRow + 16 * ((4 * c + lg) ^ (li & kMask)), kf + 4 * c);
+      const f32x4 sc = scores<D, FP8>(kf, q);
+      f32x4 f = {1, 1, 1, 1};
+      if constexpr (FP8) f = *reinterpret_cast<const f32x4*>(ks + 16 * s + 4 * lg);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = sc[r] * scale2;
+        if constexpr (FP8) x *= f[r];
+        v[4 * s + r] = tile + 16 * s + 4 * lg + r < end ? x : kNegInf;
+      }
+    }
+    bool seen[16];
+    if constexpr (FP8) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) seen[e] = !(v[e] == kNegInf);
+    }
+    online_softmax(v, m, l, o);
+    if constexpr (FP8) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(ks + 64 + 16 * s + 4 * lg);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[4 * s + r] = seen[4 * s + r] ? v[4 * s + r] * f[r] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      uint32_t vf[8][kVRow];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = 4 * lg + e % 4, at_byte = li * (kDV * kB);
+        const uint8_t* src = values + (2 * t + e / 4) * kGroup + row * kRow;
+        if constexpr (kDV * kB <= 16) {
+          load_bytes<kDV * kB>(src + 16 * ((at_byte / 16) ^ (row & kMask)) + at_byte % 16, vf[e]);
+        } else {
+          load_bytes<16>(src + 16 * ((at_byte / 16) ^ (row & kMask)), vf[e]);
+          load_bytes<16>(src + 16 * ((at_byte / 16 + 1) ^ (row & kMask)), vf[e] + 4);
+        }
+      }
+      if (tile + 64 > len) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool in = tile + 32 * t + 16 * (e / 4) + 4 * lg + e % 4 < len;
+#pragma unroll
+          for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
+        }
+      }
+      add_values<D, FP8>(vf, __builtin_bit_cast(bf16x8, pack8_bf16(v + 8 * t)), o);
+    }
+  }
+  // a wave sees its own group's pages alone
+  bad = __syncthreads_or(bad);
+  if (!busy) return;
+  if (bad) l = __builtin_nanf(""), m = 0.0f;
+  l = sum_groups(l);
+  if (col0 + li >= cols) return;
+  // a lane holds values 4 kDV lg .. of its column
+  if (direct) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + q.row * D + 4 * kDV * lg);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < kDV; j += 4)
-        *reinterpret_cast<f32x4*>(mine + r * kDV + j) = f32x4{o[n][j][r], o[n][j + 1][r], o[n][j + 2][r], o[n][j + 3][r]};
-    if (lg == 0) red_m[wave * 16 + li] = m[n], red_l[wave * 16 + li] = ln;
-    __syncthreads();
-    // thread -> (column, D / 16 values)
-    const int c = threadIdx.x / 16, d0 = (threadIdx.x % 16) * kDV;
-    const int col = (cb * NG + n) * 16 + c;
-    if (col >= cols) continue;
-    float top = red_m[c];
+        *reinterpret_cast<u32x2*>(dst + (r * kDV + j) / 2) =
+            u32x2{pack_bf16(o[j][r] * inv, o[j + 1][r] * inv), pack_bf16(o[j + 2][r] * inv, o[j + 3][r] * inv)};
+    if (a.lse != nullptr && lg == 0) a.lse[q.row] = log_sum(m, l);
+  } else {
+    const PartView pv = part_view(a.ws, static_cast<int64_t>(a.B) * a.Hk * parts * cols, D);
+    const int64_t row = ((static_cast<int64_t>(b) * a.Hk + hk) * parts + part) * cols + col0 + li;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_m[w * 16 + c]);
-    const float base = top == kNegInf ? 0.0f : top;
-    float sum = 0.0f, acc[kDV];
-#pragma unroll
-    for (int j = 0; j < kDV; ++j) acc[j] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(red_m[w * 16 + c] - base);
-      sum += f * red_l[w * 16 + c];
-#pragma unroll
-      for (int j = 0; j < kDV; ++j) acc[j] += f * red_o[(w * 16 + c) * (D + 4) + d0 + j];
-    }
-    if (direct) {
-      const int tq = col / G;
-      const int64_t row = (static_cast<int64_t>(b) * a.Tq + tq) * a.Hq + hk * G + (col - tq * G);
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      uint32_t y[kDV / 2];
-#pragma unroll
-      for (int j = 0; j < kDV / 2; ++j) y[j] = pack_bf16(acc[2 * j] * inv, acc[2 * j + 1] * inv);
-      uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D + d0);
-#pragma unroll
-      for (int j = 0; j < kDV / 2; ++j) dst[j] = y[j];
-      if (a.lse != nullptr && d0 == 0) a.lse[row] = sum == 0.0f ? kNegInf : (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
-    } else {
-      const int64_t row = ((static_cast<int64_t>(b) * a.Hk + hk) * parts + part) * cols + col;
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < kDV; j += 4)
-        *reinterpret_cast<f32x4*>(pv.o + row * D + d0 + j) = f32x4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
-      if (d0 == 0) *reinterpret_cast<float2*>(pv.ml + 2 * row) = make_float2(top, sum);
-    }
+        *reinterpret_cast<f32x4*>(pv.o + row * D + 4 * kDV * lg + r * kDV + j) =
+            f32x4{o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]};
+    if (lg == 0) *reinterpret_cast<float2*>(pv.ml + 2 * row) = make_float2(m, l);
   }
 }
 
-// Joins the parts of each query column: a block per column, D / 4 lanes of
-// four values, the rest of its 256 threads over the parts.
-template <int D>
-__global__ __launch_bounds__(256) void paged_attention_join_kernel(const AttnArgs a, int chunk, int parts) {
-  constexpr int kLanes = D / 4, kSets = 256 / kLanes;
-  __shared__ f32x4 red[kSets * kLanes];
-  __shared__ float red_s[kSets];
+// Joins the parts of the query columns.  A column's DC values (D of them, or
+// a piece of them where there are few columns) are taken by DC / 4 lanes, and
+// its parts by SETS such groups in turn; 256 threads hold 1024 / (DC * SETS)
+// columns.
+template <int D, int DC, int SETS>
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(const AttnArgs a, int chunk, int parts, int rows) {
+  constexpr int kLanes = DC / 4, kCols = 256 / (kLanes * SETS), kPieces = D / DC;
+  __shared__ f32x4 red[SETS > 1 ? 256 : 1];
+  __shared__ float red_m[SETS > 1 ? kCols * SETS : 1], red_s[SETS > 1 ? kCols * SETS : 1];
+  const int ln = threadIdx.x % kLanes, set = threadIdx.x / kLanes % SETS, c = threadIdx.x / (kLanes * SETS);
+  const int piece = blockIdx.x % kPieces, at = blockIdx.x / kPieces * kCols + c;  // [b][hk][column]
   const int G = a.Hq / a.Hk, cols = a.Tq * G;
-  int id = blockIdx.x;
-  const int col = id % cols;
-  id /= cols;
-  const int hk = id % a.Hk, b = id / a.Hk;
+  const int row_in = min(at, rows - 1);
+  const int col = row_in % cols, bh = row_in / cols, hk = bh % a.Hk, b = bh / a.Hk;
   const int len = min(a.lens[b], a.max_len);
   const int live = len > 0 ? (len + chunk - 1) / chunk : 0;
-  const PartView pv = part_view(a.ws, static_cast<int64_t>(a.B) * a.Hk * parts * cols, D);
-  const int64_t row0 = (static_cast<int64_t>(b) * a.Hk + hk) * parts * cols + col;
-  const int set = threadIdx.x / kLanes, ln = threadIdx.x % kLanes;
+  const PartView pv = part_view(a.ws, static_cast<int64_t>(rows) * parts, D);
+  const int64_t row0 = static_cast<int64_t>(bh) * parts * cols + col;
+  const int d = piece * DC + 4 * ln;
 
-  float top = kNegInf;
-  for (int i = 0; i < live; ++i) top = fmaxf(top, pv.ml[2 * (row0 + static_cast<int64_t>(i) * cols)]);
-  const float base = top == kNegInf ? 0.0f : top;
+  // this group's parts, with a running maximum like the tokens themselves
+  float top = kNegInf, sum = 0.0f;
   f32x4 acc = {0, 0, 0, 0};
-  float sum = 0.0f;
-  for (int i = set; i < live; i += kSets) {
+#pragma unroll 4
+  for (int i = set; i < live; i += SETS) {
     const int64_t row = row0 + static_cast<int64_t>(i) * cols;
     const float2 ml = *reinterpret_cast<const float2*>(pv.ml + 2 * row);
-    const float f = __builtin_amdgcn_exp2f(ml.x - base);
-    sum += f * ml.y;
-    acc += f * *reinterpret_cast<const f32x4*>(pv.o + row * D + 4 * ln);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(pv.o + row * D + d);
+    const float next = fmaxf(top, ml.x);
+    const float base = next == kNegInf ? 0.0f : next;
+    const float keep = __builtin_amdgcn_exp2f(top - base), f = __builtin_amdgcn_exp2f(ml.x - base);
+    sum = sum * keep + f * ml.y;
+    acc = acc * keep + f * v;
+    top = next;
   }
-  red[threadIdx.x] = acc;
-  if (ln == 0) red_s[set] = sum;
-  __syncthreads();
-  if (set) return;
-  sum = red_s[0];
-  for (int s = 1; s < kSets; ++s) {
-    acc += red[s * kLanes + ln];
-    sum += red_s[s];
+  if constexpr (SETS > 1) {
+    red[threadIdx.x] = acc;
+    if (ln == 0) red_m[c * SETS + set] = top, red_s[c * SETS + set] = sum;
+    __syncthreads();
+    if (set) return;
+    const float* m = red_m + c * SETS;
+    for (int s = 1; s < SETS; ++s) top = fmaxf(top, m[s]);
+    const float base = top == kNegInf ? 0.0f : top;
+    sum = 0.0f;
+    acc = f32x4{0, 0, 0, 0};
+    for (int s = 0; s < SETS; ++s) {
+      const float f = __builtin_amdgcn_exp2f(m[s] - base);
+      sum += f * red_s[c * SETS + s];
+      acc += f * red[(c * SETS + s) * kLanes + ln];
+    }
   }
+  if (at >= rows) return;
   const int tq = col / G;
   const int64_t row = (static_cast<int64_t>(b) * a.Tq + tq) * a.Hq + hk * G + (col - tq * G);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  *reinterpret_cast<u32x2*>(a.out + row * D + 4 * ln) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
-  if (a.lse != nullptr && ln == 0) a.lse[row] = sum == 0.0f ? kNegInf : (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
+  *reinterpret_cast<u32x2*>(a.out + row * D + d) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+  if (a.lse != nullptr && d == 0) a.lse[row] = log_sum(top, sum);
 }
 
-template <int D, bool FP8, int NG, int WPS>
-hipError_t launch_ng(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const int cols = a.Tq * (a.Hq / a.Hk);
-  const int col_blocks = (cols + 16 * NG - 1) / (16 * NG);
-  const int64_t blocks = static_cast<int64_t>(a.B) * a.Hk * p.parts * col_blocks;
-  hipLaunchKernelGGL((paged_attention_kernel<D, FP8, NG, WPS>), dim3(static_cast<unsigned>(blocks)), dim3(64 * kWaves), 0,
-                     st, a, p.chunk, p.parts, col_blocks);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.parts == 1) return e;
-  const int64_t rows = static_cast<int64_t>(a.B) * a.Hk * cols;
-  hipLaunchKernelGGL((paged_attention_join_kernel<D>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, p.chunk,
-                     p.parts);
+template <int D>
+hipError_t launch_join(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+  const int rows = a.B * a.Tq * a.Hq;
+#define JQ_JOIN(DC, SETS)                                                                                           \
+  {                                                                                                                 \
+    constexpr int kCols = 1024 / (DC * SETS);                                                                       \
+    hipLaunchKernelGGL((paged_attention_join_kernel<D, DC, SETS>), dim3((rows + kCols - 1) / kCols * (D / DC)),     \
+                       dim3(256), 0, st, a, p.chunk, p.parts, rows);                                                \
+  }
+  // Few columns of many parts: more threads on each, and its values over
+  // several blocks.
+  if (p.parts >= 32) JQ_JOIN(32, 32)
+  else if (p.parts >= 8 && rows < 4096) JQ_JOIN(D, (256 / D))
+  else JQ_JOIN(D, 1)
+#undef JQ_JOIN
   return hipGetLastError();
 }
 
 template <int D, bool FP8>
 hipError_t launch_d(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  constexpr int kWps = D == 256 ? 1 : 2;
-  switch (p.cols) {
-    case 16: return launch_ng<D, FP8, 1, kWps>(a, p, st);
-    case 32: return launch_ng<D, FP8, 2, kWps>(a, p, st);
-    default: return launch_ng<D, FP8, D == 256 ? 2 : 4, 1>(a, p, st);
+  const int cols = a.Tq * (a.Hq / a.Hk);
+  const int col_blocks = (cols + p.cols - 1) / p.cols;
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hk * p.parts * col_blocks)), block(64 * kWaves);
+  if (p.cols == 16) {
+    hipLaunchKernelGGL((paged_attention_kernel<D, FP8, D == 256 ? 1 : 2>), grid, block, 0, st, a, p.chunk, p.parts);
+  } else {
+    hipLaunchKernelGGL((paged_attention_wide_kernel<D, FP8, D == 256 ? 1 : 2>), grid, block, 0, st, a, p.chunk, p.parts,
+                       col_blocks);
   }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  return launch_join<D>(a, p, st);
 }
 
 }  // namespace
 
+// Parts of the key axis.  One part needs no second kernel, which costs 2.7 us;
+// a block of one part takes 1.1 us per 128 tokens, so up to three such rounds
+// stay whole.  Beyond that, enough parts to have a block for each CU (more only
+// add to what every block spends outside its loop: 1 x 131072 tokens, 8 key
+// heads: 256 blocks 96 us, 1024 99, 4096 106), and with several sequences, whose
+// lengths may differ, up to four of at least 2^18 / D tokens each (64 sequences
+// of 1 .. 8192 tokens: one part 134 us, two 122, four 115, eight 114; 64 of 4096
+// each: 101, 105, 109, 115).
 AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
   const int64_t cols = Tq * (Hq / Hk);
   AttnPlan p;
-  p.cols = cols <= 16 ? 16 : cols <= 32 || D == 256 ? 32 : 64;
+  p.cols = cols <= 16 ? 16 : 64;
   const int64_t heads = B * Hk * ((cols + p.cols - 1) / p.cols);
-  constexpr int64_t kStep = kWaves * kTile;  // a block's tokens per round
-  constexpr int64_t kBlocks = 1024;          // four blocks for each CU
-  const int64_t most = (max_len + kStep - 1) / kStep;
-  const int64_t want = std::max<int64_t>(1, std::min(most, (kBlocks + heads - 1) / heads));
-  const int64_t steps = (most + want - 1) / want;  // of a part
-  p.chunk = static_cast<int>(steps * kStep);
-  p.parts = static_cast<int>((most + steps - 1) / steps);
+  constexpr int64_t kRound = kWaves * kTile;  // tokens of a block's round; two stages of the wide kernel
+  static const int64_t kCus = getenv("JQ_BLK") ? atoi(getenv("JQ_BLK")) : 256;
+  const int64_t rounds = (max_len + kRound - 1) / kRound;
+  int64_t parts = 1;
+  if (rounds > 3) {
+    parts = (kCus + heads - 1) / heads;
+    if (B > 1) parts = std::max(parts, std::min({int64_t{4}, max_len * D >> 18, 2048 / heads}));
+    parts = std::min(parts, rounds);
+  }
+  const int64_t each = (rounds + parts - 1) / parts;
+  p.chunk = static_cast<int>(each * kRound);
+  p.parts = static_cast<int>((rounds + each - 1) / each);
   return p;
 }
 

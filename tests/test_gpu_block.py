@@ -488,6 +488,23 @@ def test_cache_beyond_32_bits(kind):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 16, 17, 33, 40, 63, 65, 300])
+def test_attention_infinite_values(n, D):
+    """An infinity in the first or last cached value is an infinity of that output element, and of no other."""
+    _say("attend infinite", n, D)
+    kc, vc, ks, vs, table, ln, g = _filled([n], 1, D, 16, "bf16", n + D)
+    q = _randn((1, 1, 3, D), g)
+    good = jb.jq_paged_attention(q, kc, vc, table, ln)
+    for t in {0, n - 1}:
+        v = vc.clone()
+        v[table[0, t // 16], 0, t % 16, 7] = -math.inf
+        out = jb.jq_paged_attention(q, kc, v, table, ln)
+        assert bool((out[..., 7] == -math.inf).all())
+        keep = torch.arange(D, device="cuda") != 7
+        assert torch.equal(out[..., keep], good[..., keep])
+
+
 # ---------------------------------------------------------------------------
 # streams and graphs
 
