@@ -28,7 +28,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <stdlib.h>
 #include <algorithm>
 #include <type_traits>
 
@@ -366,27 +365,32 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
   }
 }
 
-// More columns: a block takes 64 of them, 16 a wave, and all its waves the same
-// 64 tokens at a time, which transfers bring into LDS once for all of them,
-// each wave a group of 16, one stage ahead of the products.  A row's 16-byte
-// chunk c sits at chunk c ^ (row & 15) of its place in LDS (as far as the row
-// has chunks), so that the sixteen rows an operand spans cover all banks.
+// More columns: a block takes 64 of them, and 64 tokens at a time, which
+// transfers bring into LDS once for all its eight waves, one stage ahead of the
+// products: wave w has columns 16 (w % 4) .. and half w / 4 of the tokens.  A
+// row's 16-byte chunk c sits at chunk c ^ (row & 15) of its place in LDS (as far
+// as the row has chunks), so that the sixteen rows an operand spans cover all
+// banks.  What bounds it is the chain from a stage's rows to its outputs; four
+// waves per SIMD run theirs side by side.
+constexpr int kWideWaves = 8, kWideTile = 64;
+
 template <int D, bool FP8, int WPS>
-__global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_wide_kernel(const AttnArgs a, int chunk, int parts,
-                                                                                int col_blocks) {
+__global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_kernel(const AttnArgs a, int chunk,
+                                                                                    int parts, int col_blocks) {
   constexpr int kB = FP8 ? 1 : 2;
   constexpr int kDV = D / 16, kVRow = kDV * kB / 4;
   constexpr int kRow = D * kB;                     // bytes of a cached row
   constexpr int kChunks = kRow / 16;
   constexpr int kMask = (kChunks < 16 ? kChunks : 16) - 1;
-  constexpr int kRows = 1024 / kRow;               // rows of a transfer
   constexpr int kGroup = 16 * kRow;                // bytes of a group of 16 tokens
-  constexpr int kKeys = kWaves * kGroup, kStage = 2 * kKeys + 512;  // keys, values, their scales
-  static_assert(kRows >= 1 && kRows <= 16, "");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStage];
+  constexpr int kKeys = 4 * kGroup, kStage = 2 * kKeys + 512;  // keys, values, their scales
+  constexpr int kRedRow = 4 * kDV + 2;             // floats of a lane at the end: its outputs, maximum and sum
+  constexpr int kRed = 4 * 64 * kRedRow * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStage > kRed ? 2 * kStage : kRed];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = wave / 4;
   const int li = lane & 15, lg = lane >> 4;
   const BlockPlace at = block_place(a, col_blocks);
   const int b = at.b, hk = at.hk, part = at.part;
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_wide_kernel(
   const bool direct = parts == 1;
   if (t0 >= t1 && !direct) return;
 
-  const int col0 = 64 * at.cb + 16 * wave;
+  const int col0 = 64 * at.cb + 16 * (wave % 4);
   const bool busy = col0 < cols;  // else this wave only moves data
   Query<D, FP8> q;
   q.load(a, b, hk, min(col0 + li, cols - 1), lg);
@@ -411,46 +415,42 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_wide_kernel(
   bool bad = false;
   const uint32_t lds0 = lds_addr(lds);
 
-  // This wave's group of a stage: 16 rows that lie in one page.  Groups past the
-  // end read the stage's first one; what lies past the end counts for nothing.
+  // A stage's group that this wave moves: waves 0..3 the keys, 4..7 the values
+  // of 16 rows that lie in one page.  A group past the end reads the stage's
+  // first one; what lies past the end counts for nothing.
   auto issue = [&](int buf, int tile) __attribute__((always_inline)) {
-    const int h0 = tile + 16 * wave < len ? tile + 16 * wave : tile;
+    const int g = wave % 4;
+    const int h0 = tile + 16 * g < len ? tile + 16 * g : tile;
     int pg = table[h0 >> a.page_shift];
     if (pg < 0 || pg >= a.num_pages) bad = true, pg = 0;
     const int64_t line = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
-    const Rsrc rk = make_rsrc(static_cast<const uint8_t*>(a.k_cache) + line * kRow, kGroup);
-    const Rsrc rv = make_rsrc(static_cast<const uint8_t*>(a.v_cache) + line * kRow, kGroup);
-    const uint32_t dst = lds0 + buf * kStage + wave * kGroup;
+    const Rsrc r = make_rsrc(static_cast<const uint8_t*>(half ? a.v_cache : a.k_cache) + line * kRow, kGroup);
+    const uint32_t dst = lds0 + buf * kStage + half * kKeys + g * kGroup;
 #pragma unroll
     for (int i = 0; i < kGroup / 1024; ++i) {
-      const int row = kRows * i + lane / kChunks, c = lane % kChunks;
-      const uint32_t from = row * kRow + 16 * (c ^ (row & kMask));
-      dma16(rk, dst + 1024 * i, from, 0);
-      dma16(rv, dst + kKeys + 1024 * i, from, 0);
+      const int row = 1024 / kRow * i + lane / kChunks, c = lane % kChunks;
+      dma16(r, dst + 1024 * i, row * kRow + 16 * (c ^ (row & kMask)), 0);
     }
     if constexpr (FP8) {
-      const Rsrc rks = make_rsrc(a.k_scale + line, 64), rvs = make_rsrc(a.v_scale + line, 64);
-      const uint32_t sc = lds0 + buf * kStage + 2 * kKeys;
-      if (lane < 16) {
-        dma4(rks, sc + 64 * wave, 4 * lane, 0);
-        dma4(rvs, sc + 256 + 64 * wave, 4 * lane, 0);
-      }
+      const Rsrc rs = make_rsrc((half ? a.v_scale : a.k_scale) + line, 64);
+      if (lane < 16) dma4(rs, lds0 + buf * kStage + 2 * kKeys + 256 * half + 64 * g, 4 * lane, 0);
     }
   };
 
   if (t0 < t1) issue(0, t0);
   int buf = 0;
-  for (int tile = t0; tile < t1; tile += 64, buf ^= 1) {
+  for (int tile = t0; tile < t1; tile += kWideTile, buf ^= 1) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tile + 64 < t1) issue(buf ^ 1, tile + 64);
-    if (!busy) continue;
-    const uint8_t* keys = lds + buf * kStage;
+    if (tile + kWideTile < t1) issue(buf ^ 1, tile + kWideTile);
+    const int first = tile + 32 * half;  // of this wave's tokens
+    if (!busy || first >= t1) continue;
+    const uint8_t* keys = lds + buf * kStage + 2 * half * kGroup;
     const uint8_t* values = keys + kKeys;
-    const float* ks = reinterpret_cast<const float*>(keys + 2 * kKeys);
-    float v[16];
+    const float* ks = reinterpret_cast<const float*>(lds + buf * kStage + 2 * kKeys) + 32 * half;
+    float v[8];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < 2; ++s) {
       uint32_t kf[kRow / 16];
 #pragma unroll
       for (int c = 0; c < kRow / 64; ++c)
@@ -462,51 +462,71 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_wide_kernel(
       for (int r = 0; r < 4; ++r) {
         float x = sc[r] * scale2;
         if constexpr (FP8) x *= f[r];
-        v[4 * s + r] = tile + 16 * s + 4 * lg + r < end ? x : kNegInf;
+        v[4 * s + r] = first + 16 * s + 4 * lg + r < end ? x : kNegInf;
       }
     }
-    bool seen[16];
+    bool seen[8];
     if constexpr (FP8) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) seen[e] = !(v[e] == kNegInf);
+      for (int e = 0; e < 8; ++e) seen[e] = !(v[e] == kNegInf);
     }
     online_softmax(v, m, l, o);
     if constexpr (FP8) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+      for (int s = 0; s < 2; ++s) {
         const f32x4 f = *reinterpret_cast<const f32x4*>(ks + 64 + 16 * s + 4 * lg);
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[4 * s + r] = seen[4 * s + r] ? v[4 * s + r] * f[r] : 0.0f;
       }
     }
+    uint32_t vf[8][kVRow];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      uint32_t vf[8][kVRow];
+    for (int e = 0; e < 8; ++e) {
+      const int row = 4 * lg + e % 4, at_byte = li * (kDV * kB);
+      const uint8_t* src = values + (e / 4) * kGroup + row * kRow;
+      if constexpr (kDV * kB <= 16) {
+        load_bytes<kDV * kB>(src + 16 * ((at_byte / 16) ^ (row & kMask)) + at_byte % 16, vf[e]);
+      } else {
+        load_bytes<16>(src + 16 * ((at_byte / 16) ^ (row & kMask)), vf[e]);
+        load_bytes<16>(src + 16 * ((at_byte / 16 + 1) ^ (row & kMask)), vf[e] + 4);
+      }
+    }
+    // Rows past the end count for nothing, which an infinity times 0 would not do.
+    if (first + 32 > len) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int row = 4 * lg + e % 4, at_byte = li * (kDV * kB);
-        const uint8_t* src = values + (2 * t + e / 4) * kGroup + row * kRow;
-        if constexpr (kDV * kB <= 16) {
-          load_bytes<kDV * kB>(src + 16 * ((at_byte / 16) ^ (row & kMask)) + at_byte % 16, vf[e]);
-        } else {
-          load_bytes<16>(src + 16 * ((at_byte / 16) ^ (row & kMask)), vf[e]);
-          load_bytes<16>(src + 16 * ((at_byte / 16 + 1) ^ (row & kMask)), vf[e] + 4);
-        }
-      }
-      if (tile + 64 > len) {
+        const bool in = first + 16 * (e / 4) + 4 * lg + e % 4 < len;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool in = tile + 32 * t + 16 * (e / 4) + 4 * lg + e % 4 < len;
-#pragma unroll
-          for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
-        }
+        for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
-      add_values<D, FP8>(vf, __builtin_bit_cast(bf16x8, pack8_bf16(v + 8 * t)), o);
     }
+    add_values<D, FP8>(vf, __builtin_bit_cast(bf16x8, pack8_bf16(v)), o);
   }
-  // a wave sees its own group's pages alone
+  // a wave sees the pages of its own groups alone
   bad = __syncthreads_or(bad);
-  if (!busy) return;
+  // the second half of the tokens joins the first
+  float* red = reinterpret_cast<float*>(lds) + ((wave % 4) * kRedRow) * 64 + lane;
+  if (half) {
+#pragma unroll
+    for (int j = 0; j < kDV; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) red[64 * (4 * j + r)] = o[j][r];
+    red[64 * 4 * kDV] = m;
+    red[64 * (4 * kDV + 1)] = l;
+  }
+  __syncthreads();
+  if (half || !busy) return;
+  {
+    const float m2 = red[64 * 4 * kDV], l2 = red[64 * (4 * kDV + 1)];
+    const float top = fmaxf(m, m2), base = top == kNegInf ? 0.0f : top;
+    const float f1 = __builtin_amdgcn_exp2f(m - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
+    l = l * f1 + l2 * f2;
+    m = top;
+#pragma unroll
+    for (int j = 0; j < kDV; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[j][r] = o[j][r] * f1 + red[64 * (4 * j + r)] * f2;
+  }
   if (bad) l = __builtin_nanf(""), m = 0.0f;
   l = sum_groups(l);
   if (col0 + li >= cols) return;
@@ -615,12 +635,13 @@ template <int D, bool FP8>
 hipError_t launch_d(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const int cols = a.Tq * (a.Hq / a.Hk);
   const int col_blocks = (cols + p.cols - 1) / p.cols;
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hk * p.parts * col_blocks)), block(64 * kWaves);
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hk * p.parts * col_blocks));
   if (p.cols == 16) {
-    hipLaunchKernelGGL((paged_attention_kernel<D, FP8, D == 256 ? 1 : 2>), grid, block, 0, st, a, p.chunk, p.parts);
+    hipLaunchKernelGGL((paged_attention_kernel<D, FP8, D == 256 ? 1 : 2>), grid, dim3(64 * kWaves), 0, st, a, p.chunk,
+                       p.parts);
   } else {
-    hipLaunchKernelGGL((paged_attention_wide_kernel<D, FP8, D == 256 ? 1 : 2>), grid, block, 0, st, a, p.chunk, p.parts,
-                       col_blocks);
+    hipLaunchKernelGGL((paged_attention_wide_kernel<D, FP8, D == 256 ? 2 : 4>), grid, dim3(64 * kWideWaves), 0, st, a,
+                       p.chunk, p.parts, col_blocks);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts == 1) return e;
@@ -643,7 +664,7 @@ AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D
   p.cols = cols <= 16 ? 16 : 64;
   const int64_t heads = B * Hk * ((cols + p.cols - 1) / p.cols);
   constexpr int64_t kRound = kWaves * kTile;  // tokens of a block's round; two stages of the wide kernel
-  static const int64_t kCus = getenv("JQ_BLK") ? atoi(getenv("JQ_BLK")) : 256;
+  constexpr int64_t kCus = 256;
   const int64_t rounds = (max_len + kRound - 1) / kRound;
   int64_t parts = 1;
   if (rounds > 3) {
