@@ -110,7 +110,7 @@ def build_binding(verbose=False):
     _run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
           "-DUSE_ROCM", *[a for d in dirs for a in ("-isystem", d)], os.path.join(CSRC, BINDING_SOURCE), "-o", tmp,
           "-L", PKG, "-ljq", *[a for d in cpp_extension.library_paths() for a in ("-L", d)],
-          "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], verbose)
+          "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], verbose)
     os.replace(tmp, BINDING)
     return BINDING
 
