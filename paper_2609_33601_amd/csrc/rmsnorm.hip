@@ -28,15 +28,19 @@ namespace {
 
 using namespace block_detail;
 
-__device__ __forceinline__ u32x4 load8(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
+template <bool NT = false>
+__device__ __forceinline__ u32x4 load8(const uint16_t* p) {
+  const u32x4* q = reinterpret_cast<const u32x4*>(p);
+  return NT ? __builtin_nontemporal_load(q) : *q;
+}
 
 // h = x + residual of 8 elements, and the residual's new value.
-template <bool RES>
+template <bool RES, bool NT>
 __device__ __forceinline__ void load_h(const NormArgs& a, int64_t row, int k, float* h) {
-  unpack8_bf16(load8(a.x + row * a.x_stride + k), h);
+  unpack8_bf16(load8<NT>(a.x + row * a.x_stride + k), h);
   if constexpr (RES) {
     float r[8];
-    unpack8_bf16(load8(a.res + row * a.res_stride + k), r);
+    unpack8_bf16(load8<NT>(a.res + row * a.res_stride + k), r);
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] = h[j] + r[j];
     *reinterpret_cast<u32x4*>(a.res_out + row * a.res_out_stride + k) = pack8_bf16(h);
@@ -87,7 +91,7 @@ __device__ __forceinline__ uint32_t int4_codes(const float* y, float s) {
 }
 
 // Rows of up to 8 * LPR elements: LPR lanes a row, 256 / LPR rows a block.
-template <int LPR, NormOut OUT, bool RES>
+template <int LPR, NormOut OUT, bool RES, bool NT>
 __global__ __launch_bounds__(256) void rmsnorm_short_kernel(const NormArgs a) {
   constexpr int kRows = 256 / LPR;
   const int k = 8 * (threadIdx.x % LPR);
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(256) void rmsnorm_short_kernel(const NormArgs a) {
     const int64_t row = row0 + threadIdx.x / LPR;
     const bool in = in_row && row < a.M;
     float h[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (in) load_h<RES>(a, row, k, h);
+    if (in) load_h<RES, NT>(a, row, k, h);
     const float ss = lanes_sum<LPR>(sum_sq(h, 0.0f));
     const float r = 1.0f / sqrtf(ss / static_cast<float>(a.D) + a.eps);
     const uint32_t m = apply(h, r, w);
@@ -116,19 +120,22 @@ __global__ __launch_bounds__(256) void rmsnorm_short_kernel(const NormArgs a) {
   }
 }
 
-// Longer rows: a block takes a row, its waves NC chunks of 512 each.
-template <int NC, NormOut OUT, bool RES>
-__global__ __launch_bounds__(1024) void rmsnorm_kernel(const NormArgs a) {
+// Longer rows: a block takes a row, its waves NC chunks of 512 each; or (SOLO)
+// each of its four waves a row of its own.
+template <int NC, NormOut OUT, bool RES, bool NT, bool SOLO>
+__global__ __launch_bounds__(SOLO ? 256 : 1024) void rmsnorm_kernel(const NormArgs a) {
   __shared__ float part[16];
   __shared__ uint32_t part_max[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = SOLO ? 0 : threadIdx.x >> 6, waves = SOLO ? 1 : blockDim.x >> 6;
+  const int rows = SOLO ? 4 : 1;
   u32x4 w[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int k = (c * waves + wave) * 512 + lane * 8;
     w[c] = k < a.D ? load8(a.w + k) : u32x4{0, 0, 0, 0};
   }
-  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * rows + (SOLO ? threadIdx.x >> 6 : 0); row < a.M;
+       row += static_cast<int64_t>(gridDim.x) * rows) {
     float h[NC][8];
     float ss = 0.0f;
 #pragma unroll
@@ -136,7 +143,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_kernel(const NormArgs a) {
       const int k = (c * waves + wave) * 512 + lane * 8;
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[c][j] = 0.0f;
-      if (k < a.D) load_h<RES>(a, row, k, h[c]);
+      if (k < a.D) load_h<RES, NT>(a, row, k, h[c]);
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) ss = sum_sq(h[c], ss);
@@ -164,7 +171,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_kernel(const NormArgs a) {
         for (int i = 1; i < waves; ++i) am = umax(am, part_max[i]);
       }
       s = __uint_as_float(am) / 7.0f;
-      if (threadIdx.x == 0) a.scale[row] = s;
+      if (lane == 0 && wave == 0) a.scale[row] = s;
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -182,29 +189,43 @@ __global__ __launch_bounds__(1024) void rmsnorm_kernel(const NormArgs a) {
   }
 }
 
-template <NormOut OUT, bool RES>
+template <NormOut OUT, bool RES, bool NT>
 hipError_t launch(const NormArgs& a, hipStream_t st) {
   constexpr int64_t kMostBlocks = 1 << 20;
-  if (a.D <= 256) {
-    const int lpr = a.D <= 64 ? 8 : a.D <= 128 ? 16 : 32;
-    const int64_t blocks = (a.M + 256 / lpr - 1) / (256 / lpr);
-    const dim3 grid(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
-    if (lpr == 8) hipLaunchKernelGGL((rmsnorm_short_kernel<8, OUT, RES>), grid, dim3(256), 0, st, a);
-    else if (lpr == 16) hipLaunchKernelGGL((rmsnorm_short_kernel<16, OUT, RES>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((rmsnorm_short_kernel<32, OUT, RES>), grid, dim3(256), 0, st, a);
-    return hipGetLastError();
-  }
-  const int chunks = (a.D + 511) / 512;
-  const int per = chunks <= 2 ? 1 : chunks <= 16 ? 2 : chunks <= 64 ? 4 : 8;
-  const int waves = (chunks + per - 1) / per;
-  const dim3 grid(static_cast<unsigned>(a.M < kMostBlocks ? a.M : kMostBlocks)), block(64 * waves);
-  switch (per) {
-    case 1: hipLaunchKernelGGL((rmsnorm_kernel<1, OUT, RES>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((rmsnorm_kernel<2, OUT, RES>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((rmsnorm_kernel<4, OUT, RES>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((rmsnorm_kernel<8, OUT, RES>), grid, block, 0, st, a); break;
+  auto grid = [&](int64_t rows) {
+    const int64_t blocks = (a.M + rows - 1) / rows;
+    return dim3(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
+  };
+  if (a.D <= 64) {
+    hipLaunchKernelGGL((rmsnorm_short_kernel<8, OUT, RES, NT>), grid(32), dim3(256), 0, st, a);
+  } else if (a.D <= 128) {
+    hipLaunchKernelGGL((rmsnorm_short_kernel<16, OUT, RES, NT>), grid(16), dim3(256), 0, st, a);
+  } else if (a.D <= 256) {
+    hipLaunchKernelGGL((rmsnorm_short_kernel<32, OUT, RES, NT>), grid(8), dim3(256), 0, st, a);
+  } else {
+    // Two chunks a wave: with one, 16384 x 4096 without a residual took 48 us
+    // instead of 42, with four 45, and 4096 x 12288 66 instead of 62.
+    const int chunks = (a.D + 511) / 512;
+    if (chunks == 1) hipLaunchKernelGGL((rmsnorm_kernel<1, OUT, RES, NT, true>), grid(4), dim3(256), 0, st, a);
+    else if (chunks == 2) hipLaunchKernelGGL((rmsnorm_kernel<2, OUT, RES, NT, true>), grid(4), dim3(256), 0, st, a);
+    else if (chunks <= 32)
+      hipLaunchKernelGGL((rmsnorm_kernel<2, OUT, RES, NT, false>), grid(1), dim3(64 * ((chunks + 1) / 2)), 0, st, a);
+    else if (chunks <= 64)
+      hipLaunchKernelGGL((rmsnorm_kernel<4, OUT, RES, NT, false>), grid(1), dim3(64 * ((chunks + 3) / 4)), 0, st, a);
+    else
+      hipLaunchKernelGGL((rmsnorm_kernel<8, OUT, RES, NT, false>), grid(1), dim3(64 * ((chunks + 7) / 8)), 0, st, a);
   }
   return hipGetLastError();
+}
+
+// Inputs that the caches cannot hold anyway are read past them (non-temporal
+// loads: 16384 x 4096 46 -> 42 us, 2000 x 16384 with a residual 49 -> 42);
+// smaller ones usually lie there, as the kernel before left them (2747 x 3072:
+// 7.2 us, and 8.2 past the caches).
+template <NormOut OUT, bool RES>
+hipError_t launch(const NormArgs& a, hipStream_t st) {
+  const bool big = a.M * a.D * (RES ? 4 : 2) > (int64_t{1} << 26);
+  return big ? launch<OUT, RES, true>(a, st) : launch<OUT, RES, false>(a, st);
 }
 
 }  // namespace
