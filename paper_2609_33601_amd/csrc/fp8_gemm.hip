@@ -308,7 +308,10 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
 // Through LDS, because eight neighbouring lanes of a transfer read one row's
 // 128 bytes: a CU takes in 123 B/ns that way.  Straight into registers,
 // neighbouring lanes are the rows of an MFMA operand, 16 bytes of each, and
-// that reaches a third of it (77 x 12288 -> 4096: 55 us).
+// that reaches a third of it (77 x 12288 -> 4096: 55 us).  The path into LDS
+// bounds it: 77 x 12288 -> 4096 takes 15.9 us in 48 x 32 blocks, whose tiles of
+// X and W are 252 MB in all.  With transfers in a row it took 18.2: 10.9 of
+// them with nothing moved, 15.8 with nothing multiplied.
 
 template <int MB, int NB, int W, int S>
 __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
   constexpr int kFrags = MB + NB;                   // 16 rows x 128 bytes each
   constexpr int kOps = 2 * kFrags + 1;              // transfers of a block of k
   constexpr int kSlots = kFrags * 128 + 16;         // 16-byte slots: the fragments, then 64 scales
-  static_assert(8 % NB == 0 && (S - 1) * kOps < 64 && MB <= 4, "");
+  static_assert(8 % NB == 0 && S >= 2 && (S - 2) * kOps < 64 && MB <= 4, "");
   constexpr int kRedSlots = W * 64 * NB;  // the sums of one row group
   __shared__ uint4 lds[W * S * kSlots > kRedSlots ? W * S * kSlots : kRedSlots];
   TileCoord tc;
@@ -339,16 +342,16 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
   // step has the same number of transfers under way.
   const int chunk = (lane & 7) ^ (lane >> 3);
   const uint32_t row_at = (lane >> 3) * K + 16 * chunk;
-  auto issue = [&](int slot, int u) __attribute__((always_inline)) {
+  // Transfer i of a block of k: two of each fragment, then the scales.
+  auto issue = [&](int slot, int u, int i) __attribute__((always_inline)) {
     const uint32_t dst = ring_at + slot * kSlots * 16;
-    const bool in = u * 128 + 16 * chunk < K;
-    const uint32_t at = in ? row_at : kOutsideBuffer, so = u < kb ? u * 128 : 0;
-#pragma unroll
-    for (int f = 0; f < kFrags; ++f)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        dma16(f < NB ? rw : rx, dst + 2048 * f + 1024 * h, at + (16 * (f < NB ? f : f - NB) + 8 * h) * K, so);
-    dma4(rs, dst + 2048 * kFrags, u < kb && lane < 16 * MB ? lane * kb * 4 + u * 4 : kOutsideBuffer, 0);
+    if (i < 2 * kFrags) {
+      const int f = i / 2, h = i % 2;
+      const uint32_t at = u * 128 + 16 * chunk < K ? row_at : kOutsideBuffer;
+      dma16<0>(f < NB ? rw : rx, dst + 1024 * i, at + (16 * (f < NB ? f : f - NB) + 8 * h) * K, u < kb ? u * 128 : 0);
+    } else if (i == 2 * kFrags) {
+      dma4(rs, dst + 2048 * kFrags, u < kb && lane < 16 * MB ? lane * kb * 4 + u * 4 : kOutsideBuffer, 0);
+    }
   };
   auto frag = [&](const uint4* rows) __attribute__((always_inline)) -> i32x8 {
     const int s = li & 7;
@@ -364,19 +367,29 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
   typedef const __attribute__((address_space(4))) float* uniform_f32;
   const uniform_f32 swp = (uniform_f32)(sw + static_cast<int64_t>(n0 / 128) * kb);
 #pragma unroll
-  for (int i = 0; i < S - 1; ++i) issue(i, wave + W * i);
+  for (int i = 0; i < S - 1; ++i)
+#pragma unroll
+    for (int k = 0; k < kOps; ++k) issue(i, wave + W * i, k);
   float swv = swp[min(wave, kb - 1)];
   int slot = 0;
+  // The transfers of the block S - 1 ahead are dealt out between the products: a
+  // CU's waves share the path that takes them, and a wave that issues a block's
+  // worth in a row stands in its queue (333 x 4096 -> 4096: 16.9 us, dealt 14.9).
+  constexpr int kPer = (kOps + MB * NB) / (MB * NB + 1);
   for (int u = wave; u < kb; u += W) {
     const float sw_next = swp[min(u + W, kb - 1)];
-    // the slot before this one has been read: it takes the block S - 1 ahead
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    issue(slot == 0 ? S - 1 : slot - 1, u + W * (S - 1));
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * kOps) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * kOps) : "memory");
     const uint4* at = ring + slot * kSlots;
+    const int into = slot == 0 ? S - 1 : slot - 1, ahead = u + W * (S - 1);  // the slot before this one has been read
+    auto deal = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (kPer * step + k < kOps) issue(into, ahead, kPer * step + k);
+    };
     i32x8 w[NB];
 #pragma unroll
     for (int a = 0; a < NB; ++a) w[a] = frag(at + 128 * a);
+    deal(0);
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
       const i32x8 x = frag(at + 128 * (NB + b));
@@ -386,6 +399,7 @@ __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
         const f32x4 p = mfma128(w[a], x);
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[a][b][r] = fmaf(p[r], s, acc[a][b][r]);
+        deal(1 + b * NB + a);
       }
     }
     swv = sw_next;
@@ -417,20 +431,20 @@ namespace {
 // a launch, each round of resident blocks, and each block of 128 k that a
 // wave walks, once per round and once per block that the busiest CU has.
 // Fitted to 150 shapes (M 1 .. 2048, K 256 .. 16384, N 64 .. 16384, over their
-// logarithms) to 6 to 10% each, the tiled kernels to 17%; the kernel with the
-// lowest estimate was 1% slower than the best one on average, 19% at worst.
-// 77 x 12288 -> 4096 takes 17 us with 48 x 32 blocks and 55 us with 16 x 16
-// ones; 1 x 12288 -> 4096 takes 10 us with 16 x 16 blocks and 45 with 64 x 64.
+// logarithms) to 9 to 16% each, the tiled kernels to 18%; the kernel with the
+// lowest estimate was 2% slower than the best of 19 on average, 18% at worst.
+// 77 x 12288 -> 4096 takes 16 us with 48 x 32 blocks and 27 with 16 x 16 ones;
+// 1 x 12288 -> 4096 takes 9.5 us with 16 x 16 blocks and 23 with 64 x 64.
 struct Fp8Kernel {
   int mb, nb, waves, per_cu;            // of 16 rows and columns; waves that split K; blocks on a CU
   float launch, round, round_k, each_k;
 };
 constexpr int kFp8Few = 8;  // those of fp8_few_kernel come first, then the two of fp8_gemm_kernel
 constexpr Fp8Kernel kFp8Kernels[kFp8Few + 2] = {
-    {1, 1, 4, 3, 1597, 999, 89, 181},  {1, 1, 8, 2, 1798, 776, 0, 393},   {1, 2, 4, 3, 1794, 734, 76, 287},
-    {2, 2, 4, 2, 1659, 1025, 32, 426}, {3, 2, 4, 1, 1128, 1632, 619, 0},  {2, 4, 4, 1, 995, 1844, 727, 0},
-    {3, 4, 2, 2, 105, 3447, 594, 131}, {4, 4, 4, 1, 311, 3020, 1105, 0},  {8, 8, 1, 2, 0, 3313, 0, 730},
-    {16, 16, 1, 1, 0, 4823, 1623, 0},
+    {1, 1, 8, 2, 1754, 802, 0, 403},   {1, 2, 4, 3, 1419, 900, 112, 281}, {1, 2, 4, 2, 1465, 1166, 6, 305},
+    {2, 2, 4, 1, 1099, 1572, 425, 0},  {3, 2, 4, 1, 928, 1962, 544, 0},   {2, 4, 4, 1, 825, 2164, 655, 0},
+    {3, 4, 2, 2, 0, 3279, 364, 228},   {4, 4, 4, 1, 43, 3049, 956, 0},    {8, 8, 1, 2, 0, 3298, 0, 731},
+    {16, 16, 1, 1, 0, 4794, 1627, 0},
 };
 
 }  // namespace
@@ -465,12 +479,12 @@ hipError_t launch_fp8_gemm(const uint8_t* qx, const float* sx, int64_t M, int64_
                      static_cast<int>(M), static_cast<int>(K), qw, sw, static_cast<int>(N), bias, y, tm, tn)
 #define JQ_FEW(MB, NB, W, S) JQ_FP8((fp8_few_kernel<MB, NB, W, S>), tiles, 64 * W)
   switch (r) {
-    case 0: JQ_FEW(1, 1, 4, 3); break;
-    case 1: JQ_FEW(1, 1, 8, 2); break;
-    case 2: JQ_FEW(1, 2, 4, 2); break;
-    case 3: JQ_FEW(2, 2, 4, 2); break;
-    case 4: JQ_FEW(3, 2, 4, 2); break;
-    case 5: JQ_FEW(2, 4, 4, 2); break;
+    case 0: JQ_FEW(1, 1, 8, 2); break;
+    case 1: JQ_FEW(1, 2, 4, 2); break;
+    case 2: JQ_FEW(1, 2, 4, 3); break;
+    case 3: JQ_FEW(2, 2, 4, 3); break;
+    case 4: JQ_FEW(3, 2, 4, 3); break;
+    case 5: JQ_FEW(2, 4, 4, 3); break;
     case 6: JQ_FEW(3, 4, 2, 2); break;
     case 7: JQ_FEW(4, 4, 4, 2); break;
     // these walk tiles of their own accord: as many blocks as fit the device
