@@ -47,8 +47,10 @@ constexpr float kNegInf = -__builtin_inff();
 
 // Largest over the lanes that differ in the upper two lane bits.
 __device__ __forceinline__ float max_groups(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float sum_groups(float v) {
   v += __shfl_xor(v, 16, 64);
@@ -114,10 +116,18 @@ struct Query {
     for (int c = 0; c < D / 32; ++c) {
       // which eight of a head a lane feeds to step c: with bytes, sixteen consecutive values serve two steps
       const int d = FP8 ? 64 * (c / 2) + 16 * lg + 8 * (c % 2) : 32 * c + 8 * lg;
-      f[c] = *reinterpret_cast<const bf16x8*>(a.q + row * D + d);
+      u32x4 v = *reinterpret_cast<const u32x4*>(a.q + row * D + d);
+      if (a.scale < 0.0f) v ^= 0x80008000u;  // so that scores grow with their products
+      f[c] = __builtin_bit_cast(bf16x8, v);
     }
   }
 };
+
+// What a product is multiplied with to be a power of two; 0 as next to nothing,
+// for the masked ones' sake.
+__device__ __forceinline__ float power_scale(float scale) {
+  return scale == 0.0f ? 0x1p-126f : fabsf(scale) * 1.44269504088896340736f;
+}
 
 // S^T of 16 tokens: their rows' 16-byte chunks 4 c + lg, times the queries.
 template <int D, bool FP8>
@@ -138,25 +148,31 @@ __device__ __forceinline__ f32x4 scores(const uint32_t* k, const Query<D, FP8>& 
   return s;
 }
 
-// N more scores of a lane's column (in powers of two; -inf: not seen): their
-// powers, with the running maximum, sum and output brought along.
+// N more products of a lane's column (-inf: not seen): the powers of two of
+// their scores over m, with the sum l and the output brought along.  m follows
+// the largest score only where that has grown by more than 2^8, which seldom
+// comes after a column's first tokens (16 columns would otherwise be brought
+// along in two steps of five for a thousand tokens of random scores): powers
+// then reach 2^8 and their rounding stays relative.
 template <int N, int DV>
-__device__ __forceinline__ void online_softmax(float (&v)[N], float& m, float& l, f32x4 (&o)[DV]) {
+__device__ __forceinline__ void online_softmax(float (&v)[N], float scale2, float& m, float& l, f32x4 (&o)[DV]) {
   float top = v[0];
 #pragma unroll
   for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
-  top = fmaxf(max_groups(top), m);
-  const float base = top == kNegInf ? 0.0f : top;  // nothing seen yet: every power below is 0
-  if (__any(top != m)) {
-    const float keep = __builtin_amdgcn_exp2f(m - base);
+  top = max_groups(top) * scale2;
+  const bool grown = top > m + 8.0f;
+  if (__any(grown)) {
+    const float next = grown ? top : m;
+    const float keep = __builtin_amdgcn_exp2f(m - (next == kNegInf ? 0.0f : next));
     l *= keep;
 #pragma unroll
     for (int j = 0; j < DV; ++j) o[j] *= keep;
-    m = top;
+    m = next;
   }
+  const float base = m == kNegInf ? 0.0f : m;  // nothing seen yet: every power below is 0
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    v[e] = __builtin_amdgcn_exp2f(v[e] - base);
+    v[e] = __builtin_amdgcn_exp2f(fmaf(v[e], scale2, -base));
     l += v[e];
   }
 }
@@ -218,7 +234,8 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
 #pragma unroll
   for (int j = 0; j < kDV; ++j) o[j] = f32x4{0, 0, 0, 0};
   float m = kNegInf, l = 0.0f;
-  const float scale2 = a.scale * 1.44269504088896340736f;  // exponentials are powers of two
+  const float scale2 = power_scale(a.scale);
+  const int seen_by_all = a.causal ? min(len, len - a.Tq + 1) : len;  // tokens before it are, by every column
   // read with scalar loads: uniform, and nobody writes it meanwhile
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   const uint8_t* kbase = static_cast<const uint8_t*>(a.k_cache);
@@ -279,22 +296,22 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
     for (int s = 0; s < 2; ++s) {
       const f32x4 sc = scores<D, FP8>(kf[s], q);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = sc[r] * scale2;
-        if constexpr (FP8) x *= ks[s][r];
-        v[4 * s + r] = tile + 16 * s + 4 * lg + r < end ? x : kNegInf;
-      }
+      for (int r = 0; r < 4; ++r) v[4 * s + r] = FP8 ? sc[r] * ks[s][r] : sc[r];
     }
     if constexpr (more) load_k(next);
-    bool seen[8];
-    if constexpr (FP8) {
+    const bool mask = tile + kTile > seen_by_all;
+    if (mask) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) seen[e] = !(v[e] == kNegInf);
+      for (int e = 0; e < 8; ++e) v[e] = tile + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : kNegInf;
     }
-    online_softmax(v, m, l, o);
+    online_softmax(v, scale2, m, l, o);
     if constexpr (FP8) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = seen[e] ? v[e] * vs[e / 4][e % 4] : 0.0f;
+      for (int e = 0; e < 8; ++e) v[e] *= vs[e / 4][e % 4];
+      if (mask) {  // an unseen token's scale may be anything
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : 0.0f;
+      }
     }
     // Only a wave's last step may reach past the end.  The rows read there count
     // for nothing, which an infinity times 0 would not do.
@@ -410,7 +427,8 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
 #pragma unroll
   for (int j = 0; j < kDV; ++j) o[j] = f32x4{0, 0, 0, 0};
   float m = kNegInf, l = 0.0f;
-  const float scale2 = a.scale * 1.44269504088896340736f;
+  const float scale2 = power_scale(a.scale);
+  const int seen_by_all = a.causal ? min(len, len - a.Tq + 1 + col0 / G) : len;  // tokens before it are, by every column
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   bool bad = false;
   const uint32_t lds0 = lds_addr(lds);
@@ -418,10 +436,15 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
   // A stage's group that this wave moves: waves 0..3 the keys, 4..7 the values
   // of 16 rows that lie in one page.  A group past the end reads the stage's
   // first one; what lies past the end counts for nothing.
+  auto first_row = [&](int tile) __attribute__((always_inline)) {
+    return tile + 16 * (wave % 4) < len ? tile + 16 * (wave % 4) : tile;
+  };
+  int pg_next = t0 < t1 ? table[first_row(t0) >> a.page_shift] : 0;
   auto issue = [&](int buf, int tile) __attribute__((always_inline)) {
     const int g = wave % 4;
-    const int h0 = tile + 16 * g < len ? tile + 16 * g : tile;
-    int pg = table[h0 >> a.page_shift];
+    const int h0 = first_row(tile);
+    int pg = pg_next;
+    pg_next = table[first_row(min(tile + kWideTile, len - 1)) >> a.page_shift];
     if (pg < 0 || pg >= a.num_pages) bad = true, pg = 0;
     const int64_t line = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
     const Rsrc r = make_rsrc(static_cast<const uint8_t*>(half ? a.v_cache : a.k_cache) + line * kRow, kGroup);
@@ -459,24 +482,24 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
       f32x4 f = {1, 1, 1, 1};
       if constexpr (FP8) f = *reinterpret_cast<const f32x4*>(ks + 16 * s + 4 * lg);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = sc[r] * scale2;
-        if constexpr (FP8) x *= f[r];
-        v[4 * s + r] = first + 16 * s + 4 * lg + r < end ? x : kNegInf;
-      }
+      for (int r = 0; r < 4; ++r) v[4 * s + r] = FP8 ? sc[r] * f[r] : sc[r];
     }
-    bool seen[8];
-    if constexpr (FP8) {
+    const bool mask = first + 32 > seen_by_all;
+    if (mask) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) seen[e] = !(v[e] == kNegInf);
+      for (int e = 0; e < 8; ++e) v[e] = first + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : kNegInf;
     }
-    online_softmax(v, m, l, o);
+    online_softmax(v, scale2, m, l, o);
     if constexpr (FP8) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const f32x4 f = *reinterpret_cast<const f32x4*>(ks + 64 + 16 * s + 4 * lg);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[4 * s + r] = seen[4 * s + r] ? v[4 * s + r] * f[r] : 0.0f;
+        for (int r = 0; r < 4; ++r) v[4 * s + r] *= f[r];
+      }
+      if (mask) {  // an unseen token's scale may be anything
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = first + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : 0.0f;
       }
     }
     uint32_t vf[8][kVRow];
