@@ -680,7 +680,10 @@ hipError_t launch_d(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
 // heads: 256 blocks 96 us, 1024 99, 4096 106), and with several sequences, whose
 // lengths may differ, up to four of at least 2^18 / D tokens each (64 sequences
 // of 1 .. 8192 tokens: one part 134 us, two 122, four 115, eight 114; 64 of 4096
-// each: 101, 105, 109, 115).
+// each: 101, 105, 109, 115).  Of the wide kernel a CU holds two blocks up to
+// D = 128, and several sequences get as many of four rounds or more (6 of up to
+// 12047 tokens, 96 blocks a part: three parts 90 us, six 56; 3 of up to 3922,
+// 96: 50 and 39; 16 of 2085 each, 128: two parts 34, four 35).
 AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
   const int64_t cols = Tq * (Hq / Hk);
   AttnPlan p;
@@ -692,7 +695,10 @@ AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D
   int64_t parts = 1;
   if (rounds > 3) {
     parts = (kCus + heads - 1) / heads;
-    if (B > 1) parts = std::max(parts, std::min({int64_t{4}, max_len * D >> 18, 2048 / heads}));
+    if (B > 1) {
+      parts = std::max(parts, p.cols > 16 && D <= 128 ? std::min((2 * kCus + heads - 1) / heads, rounds / 4)
+                                                      : std::min({int64_t{4}, max_len * D >> 18, 2048 / heads}));
+    }
     parts = std::min(parts, rounds);
   }
   const int64_t each = (rounds + parts - 1) / parts;
