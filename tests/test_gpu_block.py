@@ -409,6 +409,36 @@ def test_attention_several_tokens(Tq, Hq, Hk, D, causal, kind):
     _attend_and_check(q, kc, vc, ks, vs, table, ln, causal=causal)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("Tq,Hq,Hk,D,lens", [(20, 2, 2, 128, [5000, 1, 2600]), (17, 2, 1, 64, [4099, 0, 130, 3000]),
+                                             (9, 4, 2, 256, [2500, 1300])])
+def test_attention_several_tokens_of_long_caches(Tq, Hq, Hk, D, lens, kind):
+    """Many columns over key axes that are cut into parts, most of which a short sequence does not have."""
+    _say("attend long", Tq, Hq, Hk, D, kind)
+    kc, vc, ks, vs, table, ln, g = _filled(lens, Hk, D, 32, kind, Tq + D)
+    q = _randn((len(lens), Tq, Hq, D), g, 1.5)
+    out = _attend_and_check(q, kc, vc, ks, vs, table, ln)
+    assert torch.equal(out, jb.jq_paged_attention(q, kc, vc, table, ln, k_scale=ks, v_scale=vs)), "two calls differ"
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("Tq", [1, 24])
+@pytest.mark.parametrize("rate", [0.02, 0.3, -0.3])
+def test_attention_scores_that_climb(Tq, rate, kind):
+    """Scores that rise (or fall) along the keys, a little or much within a step: the running maximum keeps up."""
+    _say("attend climb", Tq, rate, kind)
+    lens = [700, 333]
+    kc, vc, ks, vs, table, ln, g = _filled(lens, 2, 64, 16, kind, 17)
+    q = 1 + _randn((2, Tq, 4, 64), g, 0.1)
+    for b, n in enumerate(lens):
+        for t in range(n):
+            row = kc[table[b, t // 16], :, t % 16]
+            row[:] = (rate * t + row.float() * 0.01).to(row.dtype) if kind == "bf16" else torch.ones_like(row.float()).to(row.dtype)
+            if kind == "fp8":
+                ks[table[b, t // 16], :, t % 16] = rate * t
+    _attend_and_check(q, kc, vc, ks, vs, table, ln, causal=False)
+
+
 def test_attention_scale_peaks_and_bounds():
     _say("attend scale")
     lens = [500, 70, 1]
