@@ -59,10 +59,17 @@ __device__ __forceinline__ f32x4 bias4(const uint16_t* bias, int n, int N) {
   return v;
 }
 
+// A row of Y may start at any even address: these stores take any alignment
+// (4691 x 304 -> 3273: 23 us, element by element 38).
+template <typename T>
+__device__ __forceinline__ void store_any(uint16_t* p, T v) {
+  __builtin_memcpy(p, &v, sizeof(T));
+}
+
 __device__ __forceinline__ void store4(uint16_t* y, int64_t row, int N, int n, f32x4 v) {
   uint16_t* p = y + row * N + n;
-  if (N % 4 == 0) {
-    *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  if (n + 4 <= N) {
+    store_any(p, u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
   // Row group b of the tile.
   auto store = [&](int b) __attribute__((always_inline)) {
     const int m = tc.tm * BM + xrow + 16 * b, n0 = tc.tn * BN + wn * (BN / WN);
-    if (N % 8 == 0 && n0 + 64 <= N) {
+    if (n0 + 64 <= N) {
       // Lane group lg holds columns 16 a + 4 lg ..; swapping registers between
       // groups gives it 8 consecutive ones of each 32, so that a store covers
       // 64 consecutive bytes of each of 16 rows instead of 32.
@@ -210,7 +217,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
           const auto q = __builtin_amdgcn_permlane16_swap(r[0], r[1], false, false);
           out[i] = q[0], out[2 + i] = q[1];
         }
-        if (m < M) *reinterpret_cast<u32x4*>(y + static_cast<int64_t>(m) * N + n0 + 32 * h + 8 * lg) = out;
+        if (m < M) store_any(y + static_cast<int64_t>(m) * N + n0 + 32 * h + 8 * lg, out);
       }
     } else if (m < M) {
 #pragma unroll
