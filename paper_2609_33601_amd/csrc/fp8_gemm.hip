@@ -437,9 +437,9 @@ namespace {
 // The kernels that a product may take, with what estimates their time in ns:
 // a launch, each round of resident blocks, and each block of 128 k that a
 // wave walks, once per round and once per block that the busiest CU has.
-// Fitted to 150 shapes (M 1 .. 2048, K 256 .. 16384, N 64 .. 16384, over their
-// logarithms) to 9 to 16% each, the tiled kernels to 18%; the kernel with the
-// lowest estimate was 2% slower than the best of 19 on average, 18% at worst.
+// Fitted to 259 shapes (M 1 .. 8192, K 256 .. 16384, N 64 .. 16384, over their
+// logarithms) to 10 to 16% each; the kernel with the lowest estimate was 0.6%
+// slower than the best one on average, 16% at worst.
 // 77 x 12288 -> 4096 takes 16 us with 48 x 32 blocks and 27 with 16 x 16 ones;
 // 1 x 12288 -> 4096 takes 9.5 us with 16 x 16 blocks and 23 with 64 x 64.
 struct Fp8Kernel {
@@ -448,10 +448,10 @@ struct Fp8Kernel {
 };
 constexpr int kFp8Few = 8;  // those of fp8_few_kernel come first, then the two of fp8_gemm_kernel
 constexpr Fp8Kernel kFp8Kernels[kFp8Few + 2] = {
-    {1, 1, 8, 2, 1754, 802, 0, 403},   {1, 2, 4, 3, 1419, 900, 112, 281}, {1, 2, 4, 2, 1465, 1166, 6, 305},
-    {2, 2, 4, 1, 1099, 1572, 425, 0},  {3, 2, 4, 1, 928, 1962, 544, 0},   {2, 4, 4, 1, 825, 2164, 655, 0},
-    {3, 4, 2, 2, 0, 3279, 364, 228},   {4, 4, 4, 1, 43, 3049, 956, 0},    {8, 8, 1, 2, 0, 3298, 0, 731},
-    {16, 16, 1, 1, 0, 4794, 1627, 0},
+    {1, 1, 8, 2, 1713, 696, 0, 425},    {1, 2, 4, 3, 1779, 551, 31, 330},  {1, 2, 4, 2, 1628, 928, 0, 318},
+    {2, 2, 4, 1, 1124, 1500, 438, 0},   {3, 2, 4, 1, 1097, 1713, 600, 0},  {2, 4, 4, 1, 1209, 1730, 713, 0},
+    {3, 4, 2, 2, 1124, 2203, 406, 227}, {4, 4, 4, 1, 1065, 2098, 1078, 0}, {8, 8, 1, 2, 1429, 1896, 205, 554},
+    {16, 16, 1, 1, 0, 4787, 1796, 0},
 };
 
 }  // namespace

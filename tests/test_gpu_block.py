@@ -190,7 +190,8 @@ GEMM_SHAPES = [(1, 16, 1), (1, 128, 16), (1, 4096, 4096), (2, 144, 33), (16, 256
                (77, 640, 1000), (100, 2048, 96), (128, 128, 128), (129, 400, 130), (200, 1024, 4096), (257, 272, 513),
                (300, 4096, 255), (1000, 528, 1030), (1111, 1152, 2222), (4100, 384, 4200), (5, 65536, 20), (2, 16, 5000),
                (200, 4096, 2100), (130, 1040, 2500), (700, 2064, 1203), (1030, 16, 2100), (513, 144, 2056),
-               (2500, 2192, 2600), (3000, 16, 4104), (37, 624, 2737), (24, 4112, 4100)]
+               (2500, 2192, 2600), (3000, 16, 4104), (37, 624, 2737), (24, 4112, 4100),
+               (4096, 400, 4096), (4352, 656, 8201)]
 
 
 @pytest.mark.parametrize("bias", [False, True])
