@@ -24,6 +24,9 @@
 //    the workspace and a second kernel joins them.
 // Scores, statistics and sums are fp32; P is rounded to bf16 for its product
 // (its sum is of the unrounded values), which is the precision of V itself.
+// One sequence of 131072 tokens, 8 key heads of 128: 96 us, 5.6 TB/s of cache;
+// 64 sequences of 1 .. 8192, 8-bit: 110 us, 4.8 TB/s; 4 blocks of 64 new tokens
+// over up to 2080, 32 key heads: 30 us, 3.3 TB/s.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -387,8 +390,11 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
 // products: wave w has columns 16 (w % 4) .. and half w / 4 of the tokens.  A
 // row's 16-byte chunk c sits at chunk c ^ (row & 15) of its place in LDS (as far
 // as the row has chunks), so that the sixteen rows an operand spans cover all
-// banks.  What bounds it is the chain from a stage's rows to its outputs; four
-// waves per SIMD run theirs side by side.
+// banks.  What bounds it is the chain from a stage's rows to its outputs (0.9 us
+// without the transfers); two blocks a CU run theirs side by side, and the
+// transfers alone would take about as long.  V read transposed out of LDS
+// instead of zipped took as long (29 us of 29), eight waves' stores of a part
+// instead of four's too.
 constexpr int kWideWaves = 8, kWideTile = 64;
 
 template <int D, bool FP8, int WPS>
