@@ -166,8 +166,8 @@ size_t jq_paged_attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Hq, int
  *                     (NULL where that is 0)
  * A page number outside [0, num_pages) among those that a sequence's length
  * reaches makes its outputs NaN.  Places past a sequence's end are not read.
- * Cached values of tokens that only some queries of a causal call see must be
- * finite: the others take them with weight 0.
+ * An infinity or NaN among a token's cached values reaches the queries that see
+ * the token, and no other.
  * D = 64, 128 or 256; Hq % Hk == 0; page_size as above;
  * max_len <= table_cols * page_size, max_len <= 2^30; B * Tq * Hq < 2^24, and so
  * the parts that the key axis is cut into, over all sequences and heads.

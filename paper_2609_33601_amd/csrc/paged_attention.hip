@@ -182,26 +182,73 @@ __device__ __forceinline__ void online_softmax(float (&v)[N], float scale2, floa
 
 // O^T += V^T P^T of 32 tokens, one MFMA per value of a lane's V rows: v[e] are
 // D / 16 consecutive values of tokens 4 lg + e % 4 of both groups of 16.
+template <bool FP8, int ROW>
+__device__ __forceinline__ f32x4 add_value(const uint32_t (*v)[ROW], int j, bf16x8 p, f32x4 o) {
+  u32x4 r;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    uint32_t x, y;  // the dwords of tokens 2h and 2h + 1 that hold value j
+    if constexpr (FP8) {
+      const uint32_t wx = v[2 * h][j / 4], wy = v[2 * h + 1][j / 4];
+      x = (j & 2) ? e4m3_pair_to_bf16<true>(wx) : e4m3_pair_to_bf16<false>(wx);
+      y = (j & 2) ? e4m3_pair_to_bf16<true>(wy) : e4m3_pair_to_bf16<false>(wy);
+    } else {
+      x = v[2 * h][j / 2];
+      y = v[2 * h + 1][j / 2];
+    }
+    r[h] = __builtin_amdgcn_perm(y, x, (j & 1) ? 0x07060302u : 0x05040100u);
+  }
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), p, o, 0, 0, 0);
+}
 template <int D, bool FP8, int ROW>
 __device__ __forceinline__ void add_values(const uint32_t (*v)[ROW], bf16x8 p, f32x4 (&o)[D / 16]) {
 #pragma unroll
-  for (int j = 0; j < D / 16; ++j) {
-    u32x4 r;
+  for (int j = 0; j < D / 16; ++j) o[j] = add_value<FP8>(v, j, p, o[j]);
+}
+
+// Whether any of a step's values is an infinity or NaN: adding one unit to an
+// exponent (bf16) or code (e4m3) that is all ones carries into its sign bit.
+template <bool FP8, int ROW>
+__device__ __forceinline__ bool any_not_finite(const uint32_t (*v)[ROW]) {
+  constexpr uint32_t kBits = FP8 ? 0x7F7F7F7Fu : 0x7F807F80u, kUnit = FP8 ? 0x01010101u : 0x00800080u;
+  uint32_t all = 0;
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      uint32_t x, y;  // the dwords of tokens 2h and 2h + 1 that hold value j
-      if constexpr (FP8) {
-        const uint32_t wx = v[2 * h][j / 4], wy = v[2 * h + 1][j / 4];
-        x = (j & 2) ? e4m3_pair_to_bf16<true>(wx) : e4m3_pair_to_bf16<false>(wx);
-        y = (j & 2) ? e4m3_pair_to_bf16<true>(wy) : e4m3_pair_to_bf16<false>(wy);
-      } else {
-        x = v[2 * h][j / 2];
-        y = v[2 * h + 1][j / 2];
-      }
-      r[h] = __builtin_amdgcn_perm(y, x, (j & 1) ? 0x07060302u : 0x05040100u);
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int i = 0; i < ROW; ++i) all |= (v[e][i] & kBits) + kUnit;
+  return __any((all & ~kBits & (FP8 ? 0x80808080u : 0x80008000u)) != 0);
+}
+
+// The same step where columns see different numbers of its tokens (`seen` of
+// the lane's column) and a value is an infinity or NaN, which a weight of 0
+// would carry into columns that do not see it: once for each number of tokens,
+// the rows from there on zeroed, and only its columns take the result.  Leaves
+// nothing for the usual product.
+template <int D, bool FP8, int ROW>
+__device__ __forceinline__ void add_values_apart(uint32_t (*v)[ROW], bf16x8& p, int seen, int lg, f32x4 (&o)[D / 16]) {
+#pragma unroll 1
+  for (int n = kTile; n > 0; --n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool in = 16 * (e / 4) + 4 * lg + e % 4 < n;
+#pragma unroll
+      for (int i = 0; i < ROW; ++i) v[e][i] = in ? v[e][i] : 0u;
     }
-    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), p, o[j], 0, 0, 0);
+    const bool mine = min(seen, kTile) == n;
+    if (!__any(mine)) continue;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const f32x4 sum = add_value<FP8>(v, j, p, o[j]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[j][r] = mine ? sum[r] : o[j][r];
+      __builtin_amdgcn_sched_barrier(0);  // seldom run: registers matter more than speed
+    }
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int i = 0; i < ROW; ++i) v[e][i] = 0u;
+  p = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
 }
 
 __device__ __forceinline__ float log_sum(float top, float sum) {
@@ -239,6 +286,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
   float m = kNegInf, l = 0.0f;
   const float scale2 = power_scale(a.scale);
   const int seen_by_all = a.causal ? min(len, len - a.Tq + 1) : len;  // tokens before it are, by every column
+  const bool apart = a.causal && a.Tq > 1;  // columns may see different numbers of tokens
   // read with scalar loads: uniform, and nobody writes it meanwhile
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   const uint8_t* kbase = static_cast<const uint8_t*>(a.k_cache);
@@ -302,7 +350,9 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
       for (int r = 0; r < 4; ++r) v[4 * s + r] = FP8 ? sc[r] * ks[s][r] : sc[r];
     }
     if constexpr (more) load_k(next);
-    const bool mask = tile + kTile > seen_by_all;
+    // Columns of at most 16 new tokens differ in a sequence's last two tiles
+    // alone, and those are the last steps of two waves (or parts).
+    const bool mask = !decltype(more)::value && tile + kTile > seen_by_all;
     if (mask) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = tile + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : kNegInf;
@@ -326,7 +376,9 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
         for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
     }
-    add_values<D, FP8>(vf, __builtin_bit_cast(bf16x8, pack8_bf16(v)), o);
+    bf16x8 p = __builtin_bit_cast(bf16x8, pack8_bf16(v));
+    if (mask && apart && any_not_finite<FP8>(vf)) add_values_apart<D, FP8>(vf, p, end - tile, lg, o);
+    add_values<D, FP8>(vf, p, o);
     if constexpr (more) load_v(next);
   };
   int tile = t0 + wave * kTile;
@@ -435,6 +487,7 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
   float m = kNegInf, l = 0.0f;
   const float scale2 = power_scale(a.scale);
   const int seen_by_all = a.causal ? min(len, len - a.Tq + 1 + col0 / G) : len;  // tokens before it are, by every column
+  const bool apart = a.causal && a.Tq > 1;  // columns may see different numbers of tokens
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   bool bad = false;
   const uint32_t lds0 = lds_addr(lds);
@@ -529,7 +582,9 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
         for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
     }
-    add_values<D, FP8>(vf, __builtin_bit_cast(bf16x8, pack8_bf16(v)), o);
+    bf16x8 p = __builtin_bit_cast(bf16x8, pack8_bf16(v));
+    if (mask && apart && any_not_finite<FP8>(vf)) add_values_apart<D, FP8>(vf, p, end - first, lg, o);
+    add_values<D, FP8>(vf, p, o);
   }
   // a wave sees the pages of its own groups alone
   bad = __syncthreads_or(bad);

@@ -519,6 +519,38 @@ def test_cache_beyond_32_bits(kind):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("Tq,Hq,Hk,D", [(2, 2, 2, 64), (16, 1, 1, 128), (4, 8, 2, 256), (4, 2, 1, 128), (17, 2, 2, 64),
+                                         (40, 3, 1, 128), (64, 2, 2, 256), (33, 2, 1, 128)])
+def test_attention_not_finite_where_some_see_it(Tq, Hq, Hk, D, kind):
+    """Values that are infinite or NaN reach the causal queries that see their token, and no other."""
+    lens = [Tq + 1, 130, 700, Tq, Tq // 2, 257 + Tq]
+    _say("attend not finite, causal", Tq, Hq, Hk, D, kind)
+    kc, vc, ks, vs, table, ln, g = _filled(lens, Hk, D, 16, kind, 3 * Tq + D)
+    q = _randn((len(lens), Tq, Hq, D), g, 1.5)
+    good = _attend_and_check(q, kc, vc, ks, vs, table, ln)
+    reached = torch.zeros(good.shape, dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens):
+        for back, h, d in ((0, 0, 3), (Tq // 2, Hk - 1, D - 1)):
+            t = n - 1 - back                                   # seen from query Tq - 1 - back on
+            if t < 0:
+                continue
+            page, place = int(table[b, t // 16]), t % 16
+            mine = reached[b, Tq - 1 - back:, h * (Hq // Hk):(h + 1) * (Hq // Hk)]
+            if kind == "bf16":
+                vc[page, h, place, d] = math.nan if back else math.inf
+                mine[..., d] = True
+            elif back:
+                vc.view(torch.uint8)[page, h, place, d] = 0xFF  # the code of NaN
+                mine[..., d] = True
+            else:
+                vs[page, h, place] = math.nan                  # of a whole row
+                mine[:] = True
+    out = jb.jq_paged_attention(q, kc, vc, table, ln, k_scale=ks, v_scale=vs)
+    assert torch.equal(out[~reached], good[~reached])
+    assert not bool(torch.isfinite(out[reached]).any())
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("n", [1, 16, 17, 33, 40, 63, 65, 300])
 def test_attention_infinite_values(n, D):
