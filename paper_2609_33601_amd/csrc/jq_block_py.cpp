@@ -14,6 +14,7 @@
 #include <torch/csrc/python_headers.h>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 
 #include <optional>
@@ -27,13 +28,21 @@ using at::Tensor;
 // One call's tensors: all on the device of the first one seen.
 class Call {
  public:
-  // The current device becomes that of `t` for the call.
-  explicit Call(PyObject* o, const char* name) {
+  // For the call, the current device becomes that of this tensor, and the
+  // current stream the one that the caller gave (None: as it is): what the call
+  // allocates then belongs to that stream, so a workspace that it lets go at the
+  // end is not handed to another stream's work while the kernels still use it.
+  Call(PyObject* o, const char* name, PyObject* stream) {
     TORCH_CHECK_TYPE(THPVariable_Check(o), name, " must be a torch.Tensor");
     const Tensor& t = THPVariable_Unpack(o);
     TORCH_CHECK_VALUE(t.is_cuda(), name, " must be on the GPU, got ", t.device());
     device_ = t.device();
     guard_.reset_device(device_);
+    if (stream != Py_None) {
+      void* given = PyLong_AsVoidPtr(stream);
+      if (given == nullptr && PyErr_Occurred()) throw python_error();
+      stream_.reset_stream(c10::hip::getStreamFromExternal(static_cast<hipStream_t>(given), device_.index()));
+    }
   }
 
   const Tensor& tensor(PyObject* o, const char* name, at::ScalarType type) const {
@@ -76,16 +85,12 @@ class Call {
     *stride = t.size(0) > 1 ? t.stride(0) : need;
     return t;
   }
-  void* stream(PyObject* given) const {
-    if (given == Py_None) return c10::hip::getCurrentHIPStream(device_.index()).stream();
-    void* s = PyLong_AsVoidPtr(given);
-    if (s == nullptr && PyErr_Occurred()) throw python_error();
-    return s;
-  }
+  void* stream() const { return c10::hip::getCurrentHIPStream(device_.index()).stream(); }
 
  private:
   at::Device device_{at::kCPU};
   c10::OptionalDeviceGuard guard_;
+  c10::hip::OptionalHIPStreamGuard stream_;
 };
 
 void* ptr(const Tensor& t) { return t.data_ptr(); }
@@ -132,7 +137,7 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 9);
   TORCH_CHECK_VALUE(a[3] != Py_None || a[7] == Py_None, "residual_out without a residual");
-  Call c(a[0], "x");
+  Call c(a[0], "x", a[8]);
   const Tensor& x = matrix(c.tensor(a[0], "x", kBf16), "x");
   const int64_t M = x.size(0), D = x.size(1), out = integer(a[4]);
   int64_t xs = 0, rs = 0, ros = 0;
@@ -153,7 +158,7 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   const jq_status st = jq_rmsnorm(ptr(x), xs, rp, rs, ptr(w), M, D, static_cast<float>(number(a[2])),
                                   static_cast<jq_norm_out>(out), ptr(y), scale.defined() ? f32(scale) : nullptr,
-                                  res ? ptr(res_out) : nullptr, ros, c.stream(a[8]));
+                                  res ? ptr(res_out) : nullptr, ros, c.stream());
   if (st != JQ_OK) return refused(st);
   PyObject* r = PyTuple_New(1 + scale.defined() + res);
   if (r == nullptr) throw python_error();
@@ -169,13 +174,13 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* quantize_act_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 4);
-  Call c(a[0], "x");
+  Call c(a[0], "x", a[3]);
   const Tensor& x = matrix(c.tensor(a[0], "x", kBf16), "x");
   const int64_t M = x.size(0), K = x.size(1);
   int64_t xs = 0;
   c.rows(a[0], "x", x.sizes(), &xs);
   Tensor q = c.out(a[1], "q", kFp8, {M, K}), s = c.out(a[2], "scale", kF32, {M, blocks(K)});
-  const jq_status st = jq_quantize_act_fp8(ptr(x), xs, M, K, ptr(q), f32(s), c.stream(a[3]));
+  const jq_status st = jq_quantize_act_fp8(ptr(x), xs, M, K, ptr(q), f32(s), c.stream());
   return st == JQ_OK ? wrap(q, s) : refused(st);
   END_HANDLE_TH_ERRORS
 }
@@ -184,11 +189,11 @@ PyObject* quantize_act_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* pack_weight_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 4);
-  Call c(a[0], "w");
+  Call c(a[0], "w", a[3]);
   const Tensor& w = matrix(c.dense(a[0], "w", kBf16), "w");
   const int64_t N = w.size(0), K = w.size(1);
   Tensor q = c.out(a[1], "wq", kFp8, {N, K}), s = c.out(a[2], "w_scale", kF32, {blocks(N), blocks(K)});
-  const jq_status st = jq_pack_weight_fp8(ptr(w), N, K, ptr(q), f32(s), c.stream(a[3]));
+  const jq_status st = jq_pack_weight_fp8(ptr(w), N, K, ptr(q), f32(s), c.stream());
   return st == JQ_OK ? wrap(q, s) : refused(st);
   END_HANDLE_TH_ERRORS
 }
@@ -211,13 +216,13 @@ Weight weight(const Call& c, PyObject* wq, PyObject* ws, PyObject* bias, int64_t
 PyObject* fp8_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 7);
-  Call c(a[0], "q");
+  Call c(a[0], "q", a[6]);
   const Tensor& q = matrix(c.dense(a[0], "q", kFp8), "q");
   const int64_t M = q.size(0), K = q.size(1);
   const Tensor& s = c.dense(a[1], "scale", kF32, {M, blocks(K)});
   const Weight w = weight(c, a[2], a[3], a[4], K);
   Tensor y = c.out(a[5], "y", kBf16, {M, w.N});
-  const jq_status st = jq_fp8_gemm(ptr(q), f32(s), M, K, ptr(w.q), f32(w.s), w.N, w.bias, ptr(y), c.stream(a[6]));
+  const jq_status st = jq_fp8_gemm(ptr(q), f32(s), M, K, ptr(w.q), f32(w.s), w.N, w.bias, ptr(y), c.stream());
   return st == JQ_OK ? wrap(y) : refused(st);
   END_HANDLE_TH_ERRORS
 }
@@ -226,7 +231,7 @@ PyObject* fp8_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 7);
-  Call c(a[0], "x");
+  Call c(a[0], "x", a[6]);
   const Tensor& x = matrix(c.tensor(a[0], "x", kBf16), "x");
   const int64_t M = x.size(0), K = x.size(1);
   int64_t xs = 0;
@@ -236,7 +241,7 @@ PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Tensor ws = a[5] == Py_None ? c.make(at::kByte, {static_cast<int64_t>(jq_fp8_workspace_bytes(M, K))})
                               : c.dense(a[5], "workspace", at::kByte);
   const jq_status st = jq_fp8_linear(ptr(x), xs, M, K, ptr(w.q), f32(w.s), w.N, w.bias, ptr(y), ptr(ws), ws.numel(),
-                                     c.stream(a[6]));
+                                     c.stream());
   return st == JQ_OK ? wrap(y) : refused(st);
   END_HANDLE_TH_ERRORS
 }
@@ -275,7 +280,7 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 14);
   const at::ScalarType type = cache_type(a[7], a[9], a[10]);
-  Call c(a[1], "k");
+  Call c(a[1], "k", a[13]);
   const Cache kv = cache(c, type, a[7], a[8], a[9], a[10]);
   const Tensor& k = c.tensor(a[1], "k", kBf16);
   TORCH_CHECK_VALUE(k.dim() == 3, "k must be [T, Hk, D], got shape ", k.sizes());
@@ -308,7 +313,7 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const jq_status st = jq_rope_append(
       qp, qs, ptr(k), ks, ptr(v), vs, T, Hq, kv.Hk, kv.D, static_cast<const int32_t*>(ptr(pos)), cos, sin, P, R,
       truth(a[11]), static_cast<const int64_t*>(ptr(slots)), q_out.defined() ? ptr(q_out) : nullptr, qos, ptr(kv.k),
-      ptr(kv.v), kv.ks, kv.vs, kv.pages, kv.page, kv.type, c.stream(a[13]));
+      ptr(kv.v), kv.ks, kv.vs, kv.pages, kv.page, kv.type, c.stream());
   if (st != JQ_OK) return refused(st);
   if (q_out.defined()) return wrap(q_out);
   Py_RETURN_NONE;
@@ -320,7 +325,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   count(n, 14);
   const at::ScalarType type = cache_type(a[1], a[5], a[6]);
-  Call c(a[0], "q");
+  Call c(a[0], "q", a[13]);
   const Cache kv = cache(c, type, a[1], a[2], a[5], a[6]);
   const Tensor& q = c.dense(a[0], "q", kBf16);
   TORCH_CHECK_VALUE(q.dim() == 4, "q must be [B, Tq, Hq, D], got shape ", q.sizes());
@@ -343,7 +348,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       ptr(q), ptr(kv.k), ptr(kv.v), kv.ks, kv.vs, static_cast<const int32_t*>(ptr(table)), table.size(1),
       static_cast<const int32_t*>(ptr(lens)), B, Tq, Hq, kv.Hk, D, kv.pages, kv.page, max_len,
       static_cast<float>(scale), truth(a[9]), kv.type, ptr(out), lse, ws.defined() ? ptr(ws) : nullptr,
-      ws.defined() ? ws.numel() : 0, c.stream(a[13]));
+      ws.defined() ? ws.numel() : 0, c.stream());
   return st == JQ_OK ? wrap(out) : refused(st);
   END_HANDLE_TH_ERRORS
 }

@@ -7,7 +7,8 @@ jq.py, a call only turns GPU torch tensors into pointers and the current HIP
 stream (of the device that its tensors are on) and raises on a non-OK status;
 there is no other path.  The checks themselves are compiled (_jq_block.so,
 csrc/jq_block_py.cpp): TypeError for a wrong type, ValueError for a wrong shape
-or place, JQError for what the library refuses.
+or place, JQError for what the library refuses.  A call given a stream runs as
+under torch.cuda.stream(stream): what it allocates belongs to that stream.
 
     cache    k_cache, v_cache  [pages, Hk, page_size, D]  bf16, or float8_e4m3fn with
              k_scale, v_scale  [pages, Hk, page_size]     fp32 for each token and head

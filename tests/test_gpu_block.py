@@ -572,6 +572,40 @@ def test_attention_infinite_values(n, D):
 # streams and graphs
 
 
+def test_given_stream_owns_what_a_call_allocates():
+    """Outputs and workspaces of a call with a stream come from that stream's memory, so nobody else gets them early."""
+    _say("given stream")
+    g = _gen(18)
+    x = _randn((333, 1024), g)
+    wq, ws = jb.jq_pack_weight_fp8(_randn((96, 1024), g, 0.05))
+    kc, vc, ks, vs, table, ln, _ = _filled([3000, 7], 2, 64, 16, "bf16", 19)
+    q = _randn((2, 1, 4, 64), g)
+    assert jb.jq_paged_attention_workspace_bytes(2, 1, 4, 2, 64, 3008) > 0
+    want = jb.jq_fp8_linear(x, wq, ws), jb.jq_paged_attention(q, kc, vc, table, ln)
+    y, out = torch.empty_like(want[0]), torch.empty_like(want[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+    def owned():
+        return sum(s["total_size"] for s in torch.cuda.memory_snapshot() if s["stream"] == side.cuda_stream)
+
+    assert owned() == 0
+    jb.jq_fp8_linear(x, wq, ws, y=y, stream=side)
+    assert owned() > 0
+    side.synchronize()
+    torch.cuda.empty_cache()
+    jb.jq_paged_attention(q, kc, vc, table, ln, out=out, stream=side)
+    assert owned() > 0
+    side.synchronize()
+    assert torch.cuda.current_stream() != side
+    assert torch.equal(y, want[0]) and torch.equal(out, want[1])
+    norm = jb.jq_rmsnorm(x, x[0].contiguous(), stream=side)[0]
+    side.synchronize()
+    assert torch.equal(norm, jb.jq_rmsnorm(x, x[0].contiguous())[0])
+
+
 def test_other_stream_and_graph():
     """The whole chain on another stream, and captured: each replay equals the eager result."""
     _say("stream and graph")
