@@ -14,7 +14,7 @@
  *
  * e4m3 is the 8-bit float without infinities (largest 448), one byte a code.
  * A scale of a set of values v is
- *     s = max(fl32(max|v| / 448), 2^-126),  or 0 where every v is 0,
+ *     s = max(fl32(max|v| * fl32(1 / 448)), 2^-126),  or 0 where every v is 0,
  * and its codes are rne_e4m3(fl32(v / s)), 0 where s = 0.  An
  * infinity or NaN among the values makes the scale an infinity or NaN, so it
  * shows in whatever is computed from the codes.

@@ -51,12 +51,12 @@ __device__ __forceinline__ u32x2 pack8_e4m3(const float* f) {
   return r;
 }
 
-// The scale of values whose largest magnitude has these bits: a / 448, at
+// The scale of values whose largest magnitude has these bits: a (1 / 448), at
 // least 2^-126 so that its reciprocal is finite; 0 where all are 0.  Bits of
 // magnitudes order like the magnitudes with NaN on top, so an infinity or NaN
 // among the values makes the scale one, and every product with it too.
 __device__ __forceinline__ float e4m3_scale(uint32_t amax_bits) {
-  float s = __uint_as_float(amax_bits) / 448.0f;
+  float s = __uint_as_float(amax_bits) * (1.0f / 448.0f);
   if (s < 0x1p-126f) s = amax_bits == 0 ? 0.0f : 0x1p-126f;
   return s;
 }

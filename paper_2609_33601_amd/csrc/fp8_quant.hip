@@ -1,7 +1,7 @@
 // e4m3 quantisers of the 8-bit linear for gfx950.
 //
 //   activations: a block is 128 columns of a row (the last one may be short):
-//     s = max|x| / 448 (at least 2^-126; 0 for a block of zeros),
+//     s = max|x| (1 / 448) (at least 2^-126; 0 for a block of zeros),
 //     q = e4m3(x / s)
 //   weights (once, when a model is loaded): a block is 128 rows x 128 columns.
 //

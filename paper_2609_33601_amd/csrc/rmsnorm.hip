@@ -5,7 +5,7 @@
 //   h  = x + residual                    (fp32; residual' = bf16(h))
 //   y  = (h * r) * w,  r = 1 / sqrt(mean(h^2) + eps)
 //   bf16: rne(y)
-//   fp8:  s = max|y| / 448 per 128 columns, q = e4m3(y / s)
+//   fp8:  s = max|y| (1 / 448) per 128 columns, q = e4m3(y / s)
 //   int4: s = max|y| / 7 per row, q = clamp(rne(y / s), -8, 7), two a byte
 //
 // h and y stay in fp32 registers from the load to the one rounding at the

@@ -5,7 +5,7 @@
 //   on the pairs (i, i + R/2), or (2i, 2i + 1) if interleaved, i < R/2; the
 //   other D - R elements of a head pass unchanged.  Values are not rotated.
 //   Cache: [pages, Hk, page, D]; slot = page number * page + place in the page.
-//   bf16, or e4m3 codes with s = max|.| / 448 of each token and head.
+//   bf16, or e4m3 codes with s = max|.| (1 / 448) of each token and head.
 //
 // Bound: HBM; each element is read and written once.  A lane holds both
 // halves of eight pairs (two 16-byte loads), so the rotation is lane-local,
