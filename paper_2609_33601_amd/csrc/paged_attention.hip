@@ -22,11 +22,11 @@
 //    four waves take 32-token tiles in turn, each with its own running
 //    softmax, and join in LDS.  With more than one part the parts' sums go to
 //    the workspace and a second kernel joins them.
-// Scores, statistics and sums are fp32; P is rounded to bf16 for its product
-// (its sum is of the unrounded values), which is the precision of V itself.
+// Scores, statistics and sums are fp32; P takes part in its product as the sum
+// of two bf16, so that the outputs' rounding is the only one that shows.
 // One sequence of 131072 tokens, 8 key heads of 128: 96 us, 5.6 TB/s of cache;
 // 64 sequences of 1 .. 8192, 8-bit: 110 us, 4.8 TB/s; 4 blocks of 64 new tokens
-// over up to 2080, 32 key heads: 30 us, 3.3 TB/s.
+// over up to 2080, 32 key heads: 32 us, 3.1 TB/s.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -180,10 +180,31 @@ __device__ __forceinline__ void online_softmax(float (&v)[N], float scale2, floa
   }
 }
 
-// O^T += V^T P^T of 32 tokens, one MFMA per value of a lane's V rows: v[e] are
-// D / 16 consecutive values of tokens 4 lg + e % 4 of both groups of 16.
+// A lane's eight weights as the sum of two bf16, 16 bits in all: rounded to one
+// of them, weights cost the outputs as much again as their own rounding does
+// (rms error 0.0024 instead of 0.0017).  Both parts of a weight have its sign, and
+// the second, taken of the weight and a millionth more, is 0 only where the weight
+// is, so that an infinite value stays one.
+struct Weights {
+  bf16x8 high, low;
+};
+__device__ __forceinline__ Weights split_weights(const float (&v)[8]) {
+  constexpr float kMore = 1.0f + 0x1p-20f;
+  u32x4 high, low;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t a = __float_as_uint(v[2 * j]), b = __float_as_uint(v[2 * j + 1]);
+    high[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    low[j] = pack_bf16(fmaf(v[2 * j], kMore, -bf_hi(a)), fmaf(v[2 * j + 1], kMore, -bf_hi(b)));
+  }
+  return {__builtin_bit_cast(bf16x8, high), __builtin_bit_cast(bf16x8, low)};
+}
+
+// O^T += V^T P^T of 32 tokens, two MFMAs per value of a lane's V rows: v[e] are
+// D / 16 consecutive values of tokens 4 lg + e % 4 of both groups of 16.  The
+// operand of value j, for each token of a lane.
 template <bool FP8, int ROW>
-__device__ __forceinline__ f32x4 add_value(const uint32_t (*v)[ROW], int j, bf16x8 p, f32x4 o) {
+__device__ __forceinline__ bf16x8 value_operand(const uint32_t (*v)[ROW], int j) {
   u32x4 r;
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
@@ -198,12 +219,28 @@ __device__ __forceinline__ f32x4 add_value(const uint32_t (*v)[ROW], int j, bf16
     }
     r[h] = __builtin_amdgcn_perm(y, x, (j & 1) ? 0x07060302u : 0x05040100u);
   }
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), p, o, 0, 0, 0);
+  return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 template <int D, bool FP8, int ROW>
-__device__ __forceinline__ void add_values(const uint32_t (*v)[ROW], bf16x8 p, f32x4 (&o)[D / 16]) {
+__device__ __forceinline__ void add_values(const uint32_t (*v)[ROW], const Weights& p, f32x4 (&o)[D / 16]) {
+  // Two values at a time, so that no product waits for the one before it; the
+  // compiler, left to itself, puts a value's two products next to each other.
+  constexpr int kAllButMfma = 0x496;
 #pragma unroll
-  for (int j = 0; j < D / 16; ++j) o[j] = add_value<FP8>(v, j, p, o[j]);
+  for (int j = 0; j < D / 16; j += 2) {
+    const bf16x8 a = value_operand<FP8>(v, j), b = value_operand<FP8>(v, j + 1);
+    o[j] = mfma32(a, p.low, o[j]);
+    __builtin_amdgcn_sched_barrier(kAllButMfma);
+    o[j + 1] = mfma32(b, p.low, o[j + 1]);
+    __builtin_amdgcn_sched_barrier(kAllButMfma);
+    o[j] = mfma32(a, p.high, o[j]);
+    __builtin_amdgcn_sched_barrier(kAllButMfma);
+    o[j + 1] = mfma32(b, p.high, o[j + 1]);
+    __builtin_amdgcn_sched_barrier(kAllButMfma);
+  }
 }
 
 // Whether any of a step's values is an infinity or NaN: adding one unit to an
@@ -223,9 +260,9 @@ __device__ __forceinline__ bool any_not_finite(const uint32_t (*v)[ROW]) {
 // the lane's column) and a value is an infinity or NaN, which a weight of 0
 // would carry into columns that do not see it: once for each number of tokens,
 // the rows from there on zeroed, and only its columns take the result.  Leaves
-// nothing for the usual product.
+// nothing for the usual product (a branch around that took 46 registers more).
 template <int D, bool FP8, int ROW>
-__device__ __forceinline__ void add_values_apart(uint32_t (*v)[ROW], bf16x8& p, int seen, int lg, f32x4 (&o)[D / 16]) {
+__device__ __forceinline__ void add_values_apart(uint32_t (*v)[ROW], Weights& p, int seen, int lg, f32x4 (&o)[D / 16]) {
 #pragma unroll 1
   for (int n = kTile; n > 0; --n) {
 #pragma unroll
@@ -238,7 +275,8 @@ __device__ __forceinline__ void add_values_apart(uint32_t (*v)[ROW], bf16x8& p, 
     if (!__any(mine)) continue;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
-      const f32x4 sum = add_value<FP8>(v, j, p, o[j]);
+      const bf16x8 a = value_operand<FP8>(v, j);
+      const f32x4 sum = mfma32(a, p.high, mfma32(a, p.low, o[j]));
 #pragma unroll
       for (int r = 0; r < 4; ++r) o[j][r] = mine ? sum[r] : o[j][r];
       __builtin_amdgcn_sched_barrier(0);  // seldom run: registers matter more than speed
@@ -248,7 +286,7 @@ __device__ __forceinline__ void add_values_apart(uint32_t (*v)[ROW], bf16x8& p, 
   for (int e = 0; e < 8; ++e)
 #pragma unroll
     for (int i = 0; i < ROW; ++i) v[e][i] = 0u;
-  p = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  p.high = p.low = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
 }
 
 __device__ __forceinline__ float log_sum(float top, float sum) {
@@ -376,7 +414,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
         for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
     }
-    bf16x8 p = __builtin_bit_cast(bf16x8, pack8_bf16(v));
+    Weights p = split_weights(v);
     if (mask && apart && any_not_finite<FP8>(vf)) add_values_apart<D, FP8>(vf, p, end - tile, lg, o);
     add_values<D, FP8>(vf, p, o);
     if constexpr (more) load_v(next);
@@ -449,7 +487,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
 // instead of four's too.
 constexpr int kWideWaves = 8, kWideTile = 64;
 
-template <int D, bool FP8, int WPS>
+template <int D, bool FP8, bool CAUSAL, int WPS>
 __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_kernel(const AttnArgs a, int chunk,
                                                                                     int parts, int col_blocks) {
   constexpr int kB = FP8 ? 1 : 2;
@@ -480,14 +518,13 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
   const bool busy = col0 < cols;  // else this wave only moves data
   Query<D, FP8> q;
   q.load(a, b, hk, min(col0 + li, cols - 1), lg);
-  const int end = a.causal ? min(len, len - a.Tq + 1 + q.token) : len;
+  const int end = CAUSAL ? min(len, len - a.Tq + 1 + q.token) : len;
   f32x4 o[kDV];
 #pragma unroll
   for (int j = 0; j < kDV; ++j) o[j] = f32x4{0, 0, 0, 0};
   float m = kNegInf, l = 0.0f;
   const float scale2 = power_scale(a.scale);
-  const int seen_by_all = a.causal ? min(len, len - a.Tq + 1 + col0 / G) : len;  // tokens before it are, by every column
-  const bool apart = a.causal && a.Tq > 1;  // columns may see different numbers of tokens
+  const int seen_by_all = CAUSAL ? min(len, len - a.Tq + 1 + col0 / G) : len;  // tokens before it are, by every column
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   bool bad = false;
   const uint32_t lds0 = lds_addr(lds);
@@ -582,8 +619,10 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
         for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
     }
-    bf16x8 p = __builtin_bit_cast(bf16x8, pack8_bf16(v));
-    if (mask && apart && any_not_finite<FP8>(vf)) add_values_apart<D, FP8>(vf, p, end - first, lg, o);
+    Weights p = split_weights(v);
+    if constexpr (CAUSAL) {  // columns may see different numbers of tokens
+      if (mask && any_not_finite<FP8>(vf)) add_values_apart<D, FP8>(vf, p, end - first, lg, o);
+    }
     add_values<D, FP8>(vf, p, o);
   }
   // a wave sees the pages of its own groups alone
@@ -724,8 +763,14 @@ hipError_t launch_d(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
     hipLaunchKernelGGL((paged_attention_kernel<D, FP8, D == 256 ? 1 : 2>), grid, dim3(64 * kWaves), 0, st, a, p.chunk,
                        p.parts);
   } else {
-    hipLaunchKernelGGL((paged_attention_wide_kernel<D, FP8, D == 256 ? 2 : 4>), grid, dim3(64 * kWideWaves), 0, st, a,
-                       p.chunk, p.parts, col_blocks);
+    constexpr int kWps = D == 256 ? 2 : 4;
+    if (a.causal) {
+      hipLaunchKernelGGL((paged_attention_wide_kernel<D, FP8, true, kWps>), grid, dim3(64 * kWideWaves), 0, st, a,
+                         p.chunk, p.parts, col_blocks);
+    } else {
+      hipLaunchKernelGGL((paged_attention_wide_kernel<D, FP8, false, kWps>), grid, dim3(64 * kWideWaves), 0, st, a,
+                         p.chunk, p.parts, col_blocks);
+    }
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts == 1) return e;

@@ -551,6 +551,20 @@ def test_attention_not_finite_where_some_see_it(Tq, Hq, Hk, D, kind):
     assert not bool(torch.isfinite(out[reached]).any())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("Tq,Hq,Hk,D", [(1, 8, 2, 128), (1, 4, 4, 64), (2, 8, 1, 256), (64, 2, 2, 128)])
+def test_attention_error_is_the_outputs_rounding(Tq, Hq, Hk, D, kind):
+    """Weights have 16 bits in their product, so that the outputs' rounding to 8 is the only one that shows: the rms error
+    is that of the rounded 64-bit result, within a tenth."""
+    _say("attend error", Tq, Hq, Hk, D, kind)
+    lens = [2000, 333]
+    kc, vc, ks, vs, table, ln, g = _filled(lens, Hk, D, 16, kind, 23)
+    q = _randn((2, Tq, Hq, D), g, 1.5)
+    want = ref.attention(q, kc, vc, table, ln, ks, vs)[0]
+    out = jb.jq_paged_attention(q, kc, vc, table, ln, k_scale=ks, v_scale=vs).double()
+    assert float((out - want).norm()) <= 1.1 * float((want.bfloat16().double() - want).norm())
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("n", [1, 16, 17, 33, 40, 63, 65, 300])
 def test_attention_infinite_values(n, D):
