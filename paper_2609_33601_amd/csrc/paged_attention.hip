@@ -329,6 +329,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
   const uint8_t* kbase = static_cast<const uint8_t*>(a.k_cache);
   const uint8_t* vbase = static_cast<const uint8_t*>(a.v_cache);
+  const uint32_t num_pages = static_cast<uint32_t>(a.num_pages);  // below 2^31
   bool bad = false;  // a page number outside the cache was met
 
   // A step's place: the first cached row of each group of 16 tokens, and the
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
     for (int s = 0; s < 2; ++s) {
       const int h0 = tile + 16 * s < len ? tile + 16 * s : tile;
       int pg = table[h0 >> a.page_shift];
-      if (pg < 0 || pg >= a.num_pages) bad = true, pg = 0;
+      if (static_cast<uint32_t>(pg) >= num_pages) bad = true, pg = 0;
       p.line[s] = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
       p.last[s] = min(len - 1 - h0, 15);
     }
@@ -391,9 +392,10 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
     // Columns of at most 16 new tokens differ in a sequence's last two tiles
     // alone, and those are the last steps of two waves (or parts).
     const bool mask = !decltype(more)::value && tile + kTile > seen_by_all;
+    const int left = end - tile - 4 * lg, in_len = len - tile - 4 * lg;  // from the lane's first token on
     if (mask) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = tile + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : kNegInf;
+      for (int e = 0; e < 8; ++e) v[e] = 16 * (e / 4) + e % 4 < left ? v[e] : kNegInf;
     }
     online_softmax(v, scale2, m, l, o);
     if constexpr (FP8) {
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
       for (int e = 0; e < 8; ++e) v[e] *= vs[e / 4][e % 4];
       if (mask) {  // an unseen token's scale may be anything
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tile + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = 16 * (e / 4) + e % 4 < left ? v[e] : 0.0f;
       }
     }
     // Only a wave's last step may reach past the end.  The rows read there count
@@ -409,7 +411,7 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
     if constexpr (!more) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool in = tile + 16 * (e / 4) + 4 * lg + e % 4 < len;
+        const bool in = 16 * (e / 4) + e % 4 < in_len;
 #pragma unroll
         for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
@@ -526,6 +528,7 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
   const float scale2 = power_scale(a.scale);
   const int seen_by_all = CAUSAL ? min(len, len - a.Tq + 1 + col0 / G) : len;  // tokens before it are, by every column
   const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(b) * a.table_cols);
+  const uint32_t num_pages = static_cast<uint32_t>(a.num_pages);  // below 2^31
   bool bad = false;
   const uint32_t lds0 = lds_addr(lds);
 
@@ -541,7 +544,7 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
     const int h0 = first_row(tile);
     int pg = pg_next;
     pg_next = table[first_row(min(tile + kWideTile, len - 1)) >> a.page_shift];
-    if (pg < 0 || pg >= a.num_pages) bad = true, pg = 0;
+    if (static_cast<uint32_t>(pg) >= num_pages) bad = true, pg = 0;
     const int64_t line = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (h0 & (page - 1));
     const Rsrc r = make_rsrc(static_cast<const uint8_t*>(half ? a.v_cache : a.k_cache) + line * kRow, kGroup);
     const uint32_t dst = lds0 + buf * kStage + half * kKeys + g * kGroup;
@@ -581,9 +584,10 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
       for (int r = 0; r < 4; ++r) v[4 * s + r] = FP8 ? sc[r] * f[r] : sc[r];
     }
     const bool mask = first + 32 > seen_by_all;
+    const int left = end - first - 4 * lg, in_len = len - first - 4 * lg;  // from the lane's first token on
     if (mask) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = first + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : kNegInf;
+      for (int e = 0; e < 8; ++e) v[e] = 16 * (e / 4) + e % 4 < left ? v[e] : kNegInf;
     }
     online_softmax(v, scale2, m, l, o);
     if constexpr (FP8) {
@@ -595,7 +599,7 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
       }
       if (mask) {  // an unseen token's scale may be anything
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = first + 16 * (e / 4) + 4 * lg + e % 4 < end ? v[e] : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = 16 * (e / 4) + e % 4 < left ? v[e] : 0.0f;
       }
     }
     uint32_t vf[8][kVRow];
@@ -614,7 +618,7 @@ __global__ __launch_bounds__(64 * kWideWaves, WPS) void paged_attention_wide_ker
     if (first + 32 > len) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool in = first + 16 * (e / 4) + 4 * lg + e % 4 < len;
+        const bool in = 16 * (e / 4) + e % 4 < in_len;
 #pragma unroll
         for (int i = 0; i < kVRow; ++i) vf[e][i] = in ? vf[e][i] : 0u;
       }
