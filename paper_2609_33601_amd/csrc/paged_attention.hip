@@ -26,7 +26,7 @@
 // of two bf16, so that the outputs' rounding is the only one that shows.
 // One sequence of 131072 tokens, 8 key heads of 128: 96 us, 5.6 TB/s of cache;
 // 64 sequences of 1 .. 8192, 8-bit: 110 us, 4.8 TB/s; 4 blocks of 64 new tokens
-// over up to 2080, 32 key heads: 32 us, 3.1 TB/s.
+// over up to 2080, 32 key heads: 32 us, 3.2 TB/s.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
