@@ -60,15 +60,24 @@ __device__ __forceinline__ float e4m3_scale(uint32_t amax_bits) {
   if (s < 0x1p-126f) s = amax_bits == 0 ? 0.0f : 0x1p-126f;
   return s;
 }
-__device__ __forceinline__ float e4m3_inv(float s) { return s == 0.0f ? 0.0f : 1.0f / s; }
+// What e4m3_quotient divides by, with its rounded reciprocal.  For a scale of 0
+// (whose values are all 0) and for an infinite one both are 0: v / inf is 0 for
+// a finite v and NaN for an infinite one, and so is v times 0.
+struct E4m3Divisor {
+  float s, inv;
+};
+__device__ __forceinline__ E4m3Divisor e4m3_divisor(float s) {
+  const float d = __float_as_uint(s) == 0x7F800000u ? 0.0f : s;
+  return {d, d == 0.0f ? 0.0f : 1.0f / d};
+}
 
-// fl32(v / s) from inv = fl32(1 / s), three operations instead of a division's
-// ten: the remainder of v * inv is exact in one fma, and adding it times inv
-// rounds correctly because inv is the rounded reciprocal (Markstein).  bf16
-// inputs meet ties of e4m3 too often for a quotient that is an ulp off.
-__device__ __forceinline__ float e4m3_quotient(float v, float s, float inv) {
-  const float q = v * inv;
-  return fmaf(fmaf(-q, s, v), inv, q);
+// fl32(v / s) from the rounded reciprocal of s, three operations instead of a
+// division's ten: the remainder of v * inv is exact in one fma, and adding it
+// times inv rounds correctly because inv is the rounded reciprocal (Markstein).
+// bf16 inputs meet ties of e4m3 too often for a quotient that is an ulp off.
+__device__ __forceinline__ float e4m3_quotient(float v, E4m3Divisor d) {
+  const float q = v * d.inv;
+  return fmaf(fmaf(-q, d.s, v), d.inv, q);
 }
 
 // The value of another lane of the same row of 16 (DPP), all lanes taking part.

@@ -41,10 +41,10 @@ __global__ __launch_bounds__(256) void quantize_fp8_kernel(const uint16_t* __res
     float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (in) unpack8_bf16(*reinterpret_cast<const u32x4*>(x + row * x_stride + k), f);
     const float s = e4m3_scale(lanes_max<16>(max8(f)));
-    const float inv = e4m3_inv(s);
+    const E4m3Divisor d = e4m3_divisor(s);
     if (!in) continue;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = e4m3_quotient(f[j], s, inv);
+    for (int j = 0; j < 8; ++j) f[j] = e4m3_quotient(f[j], d);
     *reinterpret_cast<u32x2*>(q + static_cast<int64_t>(row) * K + k) = pack8_e4m3(f);
     if (k % 128 == 0) scale[static_cast<int64_t>(row) * ((K + 127) / 128) + k / 128] = s;
   }
@@ -73,14 +73,14 @@ __global__ __launch_bounds__(256) void pack_fp8_kernel(const uint16_t* __restric
   __syncthreads();
   m = umax(umax(part[0], part[1]), umax(part[2], part[3]));
   const float s = e4m3_scale(m);
-  const float inv = e4m3_inv(s);
+  const E4m3Divisor d = e4m3_divisor(s);
   if (threadIdx.x == 0) scale[blockIdx.x] = s;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t n = nb * 128 + r0 + 16 * i;
     if (n >= N || k >= K) continue;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[i][j] = e4m3_quotient(f[i][j], s, inv);
+    for (int j = 0; j < 8; ++j) f[i][j] = e4m3_quotient(f[i][j], d);
     *reinterpret_cast<u32x2*>(q + n * K + k) = pack8_e4m3(f[i]);
   }
 }

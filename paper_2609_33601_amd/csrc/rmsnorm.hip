@@ -71,11 +71,11 @@ __device__ __forceinline__ uint32_t apply(float* h, float r, u32x4 wv) {
 template <int L>
 __device__ __forceinline__ void store_fp8(const NormArgs& a, int64_t row, int k, const float* y, uint32_t m, bool in) {
   const float s = e4m3_scale(lanes_max<L>(m));
-  const float inv = e4m3_inv(s);
+  const E4m3Divisor d = e4m3_divisor(s);
   if (!in) return;
   float t[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) t[j] = e4m3_quotient(y[j], s, inv);
+  for (int j = 0; j < 8; ++j) t[j] = e4m3_quotient(y[j], d);
   *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.y) + row * a.D + k) = pack8_e4m3(t);
   if (k % 128 == 0) a.scale[row * ((a.D + 127) / 128) + k / 128] = s;
 }

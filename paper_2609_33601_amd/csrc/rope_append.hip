@@ -94,9 +94,9 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
     const int64_t page = slot >> a.page_shift;
     const int64_t line = ((page * a.Hk + hk) << a.page_shift) + (slot & (a.page - 1));
     if constexpr (FP8) {
-      const float inv = e4m3_inv(s);
+      const E4m3Divisor d = e4m3_divisor(s);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) f[j] = e4m3_quotient(f[j], s, inv);
+      for (int j = 0; j < 16; ++j) f[j] = e4m3_quotient(f[j], d);
       uint8_t* dst = static_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache) + line * a.D;
       *reinterpret_cast<u32x2*>(dst + i0) = pack8_e4m3(f);
       *reinterpret_cast<u32x2*>(dst + i1) = pack8_e4m3(f + 8);
