@@ -256,7 +256,9 @@ struct Cache {
 // What a cache's type asks of its scales; the type.
 at::ScalarType cache_type(PyObject* ko, PyObject* kso, PyObject* vso) {
   TORCH_CHECK_TYPE(THPVariable_Check(ko), "k_cache must be a torch.Tensor");
-  if (THPVariable_Unpack(ko).scalar_type() == kBf16) {
+  const at::ScalarType type = THPVariable_Unpack(ko).scalar_type();
+  TORCH_CHECK_TYPE(type == kBf16 || type == kFp8, "k_cache must be ", kBf16, " or ", kFp8, ", got ", type);
+  if (type == kBf16) {
     TORCH_CHECK_VALUE(kso == Py_None && vso == Py_None, "a bf16 cache has no scales");
     return kBf16;
   }
