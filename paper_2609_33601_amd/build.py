@@ -97,18 +97,44 @@ def build(verbose=False, extra_flags=(), jobs=None):
     return LIB
 
 
-def build_binding(verbose=False):
-    """Compile jq_block.py's extension against the built libjq.so."""
+def binding_lacks():
+    """What jq_block.py's extension needs and this machine does not have, or None."""
     import sysconfig
 
+    try:
+        import torch
+    except ImportError:
+        return "torch is not installed"
+    if torch.version.hip is None:
+        return "torch is not built for ROCm"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h is not installed"
+    return None
+
+
+def build_binding(verbose=False):
+    """Compile jq_block.py's extension against the built libjq.so; returns its path.
+
+    libjq.so and its C ABI need none of what the extension needs: where that is missing, says so and returns None, and
+    jq_block.py raises at its first call."""
+    import sysconfig
+
+    lacks = binding_lacks()
+    if lacks is not None:
+        if os.path.exists(BINDING):  # of an earlier build
+            os.remove(BINDING)
+        print(f"{os.path.basename(BINDING)} not built: {lacks}", flush=True)
+        return None
     from torch.utils import cpp_extension
 
     rocm = os.path.dirname(os.path.dirname(hipcc()))
     dirs = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(rocm, "include"),
                                             os.path.join(ROOT, "include")]
+    cxx = shutil.which("g++")
     tmp = BINDING + ".tmp"
-    _run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
-          "-DUSE_ROCM", *[a for d in dirs for a in ("-isystem", d)], os.path.join(CSRC, BINDING_SOURCE), "-o", tmp,
+    _run([*([cxx] if cxx else [hipcc(), "-x", "c++"]), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+          "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM", *[a for d in dirs for a in ("-isystem", d)],
+          os.path.join(CSRC, BINDING_SOURCE), "-o", tmp,
           "-L", PKG, "-ljq", *[a for d in cpp_extension.library_paths() for a in ("-L", d)],
           "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], verbose)
     os.replace(tmp, BINDING)

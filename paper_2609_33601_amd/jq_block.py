@@ -65,7 +65,7 @@ class _Native:
         import torch  # noqa: F401
 
         if not os.path.exists(NATIVE_PATH):
-            raise RuntimeError(f"{NATIVE_PATH} is missing: build the HIP library first "
+            raise RuntimeError(f"{NATIVE_PATH} is missing: build the HIP library first, with torch for ROCm installed "
                                "(python -c 'import __graft_entry__ as g; g.build()')")
         lib()
         spec = importlib.util.spec_from_file_location("_jq_block", NATIVE_PATH)
