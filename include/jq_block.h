@@ -129,8 +129,11 @@ typedef enum {
  *   k_cache, v_cache   [num_pages, Hk, page_size, D], bf16 or e4m3
  *   k_scale, v_scale   [num_pages, Hk, page_size] fp32 for JQ_CACHE_FP8, else NULL
  * A token whose slot lies outside [0, num_pages * page_size), as -1 does, is
- * not appended.  A position outside [0, P) gives NaN in the rotated elements.
- * Two tokens of one call with the same slot: it holds either.
+ * not appended.  A position outside [0, P) gives NaN in the rotated elements
+ * (and, by its scale, in the whole key of an 8-bit cache).  What a slot holds
+ * that two tokens of one call share is unspecified: a token and head is written
+ * by several stores, so it may be parts of both, an 8-bit cache's codes of one
+ * beside the scale of the other.  No other slot is affected.
  * D % 16 == 0, 16 <= D <= 256; R % 16 == 0, 0 <= R <= D (cos and sin may be
  * NULL with R = 0); page_size a power of two, 16 .. 65536; strides % 8 == 0 and
  * at least a token's elements; T * (Hq + 2 Hk) < 2^31; pointers 16-byte

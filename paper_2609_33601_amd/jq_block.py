@@ -130,7 +130,8 @@ def jq_rope_append(q, k, v, positions, cos, sin, slots, k_cache, v_cache, k_scal
                    interleaved=False, q_out=None, stream=None):
     """Rotate q [T,Hq,D] and k [T,Hk,D] (bf16, tokens may be apart) by positions int32 [T] on the first R elements of
     a head (cos, sin fp32 [P,R/2]; None for R = 0), write k and v into the cache at slots int64 [T] (negative: not
-    appended), and return the rotated q (q_out=q: in place).  q = None only appends, and returns None."""
+    appended; the slots of a call differ), and return the rotated q (q_out=q: in place).  q = None only appends, and
+    returns None."""
     return _done(_native.rope_append(q, k, v, positions, cos, sin, slots, k_cache, v_cache, k_scale, v_scale,
                                      interleaved, q_out, _stream(stream)), "jq_rope_append")
 
