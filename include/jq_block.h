@@ -168,9 +168,12 @@ size_t jq_paged_attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Hq, int
  *   workspace    at least jq_paged_attention_workspace_bytes, 256-byte aligned
  *                     (NULL where that is 0)
  * A page number outside [0, num_pages) among those that a sequence's length
- * reaches makes its outputs NaN.  Places past a sequence's end are not read.
+ * reaches makes its outputs NaN; entries past those are not read.  Of a
+ * sequence's last page, places past its end may be read (up to the end of a group
+ * of 16 tokens), whatever they hold, and count for nothing.
  * An infinity or NaN among a token's cached values reaches the queries that see
- * the token, and no other.
+ * the token, and no other; a score of -infinity is a weight of 0, and a query with
+ * no other scores is as one that sees nothing.
  * D = 64, 128 or 256; Hq % Hk == 0; page_size as above;
  * max_len <= table_cols * page_size, max_len <= 2^30; B * Tq * Hq < 2^24, and so
  * the parts that the key axis is cut into, over all sequences and heads.
