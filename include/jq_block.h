@@ -47,6 +47,7 @@ typedef enum {
  * JQ_NORM_BF16 rounds y to bf16.  JQ_NORM_FP8 quantises each 128 columns of y
  * as above.  JQ_NORM_INT4 takes s = fl32(max|y| / 7) of the row and
  * clamp(rne(fl32(y / s)), -8, 7), the rule of jq_quantize_act, on the fp32 y.
+ * Where the sum of squares passes fp32's range (|h| near 2^64), r is 0.
  *   x            in   [M,D] bf16, rows x_stride elements apart
  *   residual     in   [M,D] bf16, rows residual_stride apart, or NULL
  *   weight       in   [D] bf16

@@ -8,8 +8,10 @@
 // columns n of one row m: its scale is one number per 16 rows, and its
 // outputs are one 8-byte store.
 //
-// Bound: the weights' bytes for few rows (1 x 12288 -> 4096: 9.5 us, 5.3 TB/s),
-// the path into LDS for some dozens, the matrix cores for many.
+// Bound: the weights' bytes for few rows (1 x 12288 -> 4096: 9.3 us, 5.4 TB/s,
+// where the last-level cache of 256 MB holds them, 14 us from HBM), their transfers
+// for some dozens, the chain of a wave alone on its SIMD for some hundreds, the
+// matrix cores for many.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -93,8 +95,8 @@ __device__ __forceinline__ void store4(uint16_t* y, int64_t row, int N, int n, f
 // row group are read while the two groups multiply.  Between stages, and
 // between tiles, the matrix pipe sees no gap but the stores.
 //
-// 8192 x 4096 -> 12288: 395 to 410 us, 2.0 to 2.1 PFLOP/s.  Power holds the
-// clock: the same instructions on operands that do not change from stage to
+// 8192 x 4096 -> 12288: 395 to 410 us among other calls, 2.0 to 2.1 PFLOP/s (406
+// to 463 in traces of a dozen launches).  Power holds the clock: the same instructions on operands that do not change from stage to
 // stage take 280 us, and the stores 20 to 40 of the 395.
 
 template <int BM, int BN, int WM, int WN, int WPS>
@@ -322,10 +324,13 @@ __global__ __launch_bounds__(64 * WM * WN, WPS) void fp8_gemm_kernel(
 // Through LDS, because eight neighbouring lanes of a transfer read one row's
 // 128 bytes: a CU takes in 123 B/ns that way.  Straight into registers,
 // neighbouring lanes are the rows of an MFMA operand, 16 bytes of each, and
-// that reaches a third of it (77 x 12288 -> 4096: 55 us).  The path into LDS
-// bounds it: 77 x 12288 -> 4096 takes 15.9 us in 48 x 32 blocks, whose tiles of
-// X and W are 252 MB in all.  With transfers in a row it took 18.2: 10.9 of
-// them with nothing moved, 15.8 with nothing multiplied.
+// that reaches a third of it (77 x 12288 -> 4096: 55 us).  Waiting for transfers
+// bounds it: 77 x 12288 -> 4096 takes 15.8 us in 48 x 32 blocks, and 21.5 with the
+// weights from HBM instead of the last-level cache.  With transfers in a row it
+// took 18.2: 10.9 of them with nothing moved, 15.8 with nothing multiplied.  The
+// blocks' tiles of X and W, 252 MB in all, would take 8 us at a CU's rate into LDS
+// and the weights' 50 MB 9.5 at a copy's: the rest is latency that two blocks of k
+// on their way to each wave do not cover.
 
 template <int MB, int NB, int W, int S>
 __global__ __launch_bounds__(64 * W) void fp8_few_kernel(
@@ -446,9 +451,11 @@ namespace {
 // wave walks, once per round and once per block that the busiest CU has.
 // Fitted to 259 shapes (M 1 .. 8192, K 256 .. 16384, N 64 .. 16384, over their
 // logarithms) to 10 to 16% each; the kernel with the lowest estimate was 0.6%
-// slower than the best one on average, 16% at worst.
-// 77 x 12288 -> 4096 takes 16 us with 48 x 32 blocks and 27 with 16 x 16 ones;
-// 1 x 12288 -> 4096 takes 9.5 us with 16 x 16 blocks and 23 with 64 x 64.
+// slower than the best one on average, 16% at worst; on 68 other shapes (M 1 ..
+// 4096, weights from HBM) 0.8 and 17%.
+// 96 x 4096 -> 4096 takes 9.8 us with 48 x 32 blocks, 18 with 16 x 16 ones and 32
+// with 128 x 128; 1 x 4096 -> 4096 6.1 with 16 x 16 blocks and 13 with 64 x 64;
+// 4096 x 4096 -> 4096 68 with 256 x 256 and 85 with 128 x 128.
 struct Fp8Kernel {
   int mb, nb, waves, per_cu;            // of 16 rows and columns; waves that split K; blocks on a CU
   float launch, round, round_k, each_k;

@@ -8,7 +8,7 @@
 // Bound: HBM, 2 bytes read and 1 written per element.  Activations: sixteen
 // lanes hold a block (8 elements each), so its maximum takes four DPP steps
 // and nothing passes through LDS; a wave takes 512 columns of a row.
-// 16384 x 4096: 38 us, 5.4 TB/s; 77 x 12288: 2.6 us, a launch.
+// 16384 x 4096: 37 us, 5.4 TB/s; 77 x 12288: 2.6 us, a launch.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -8,7 +8,7 @@
 //
 // What bounds it: reading the cache once.  Everything else follows from that.
 //  * Columns.  The query heads of one key head, times the new tokens, are the
-//    columns of a matrix product, 16 (or 32, 64) of them at a time, so a
+//    columns of a matrix product, 16 (or 64) of them at a time, so a
 //    cached row is read once for all of them.
 //  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 MFMAs.  With S transposed, the
 //    lane that holds a column's scores holds the same column's row of P as
@@ -26,7 +26,7 @@
 // of two bf16, so that the outputs' rounding is the only one that shows.
 // One sequence of 131072 tokens, 8 key heads of 128: 96 us, 5.6 TB/s of cache;
 // 64 sequences of 1 .. 8192, 8-bit: 110 us, 4.8 TB/s; 4 blocks of 64 new tokens
-// over up to 2080, 32 key heads: 32 us, 3.2 TB/s.
+// over up to 2080, 32 key heads: 31 us, 3.3 TB/s (36 with the cache from HBM).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -486,7 +486,9 @@ __global__ __launch_bounds__(64 * kWaves, WPS) void paged_attention_kernel(const
 // without the transfers); two blocks a CU run theirs side by side, and the
 // transfers alone would take about as long.  V read transposed out of LDS
 // instead of zipped took as long (29 us of 29), eight waves' stores of a part
-// instead of four's too.
+// instead of four's too.  A causal block walks all stages of its part, also those
+// that none of its columns see: a prompt takes about twice the stages that it
+// needs (2048 new tokens, 32 query heads on 8 key heads of 128: 146 us).
 constexpr int kWideWaves = 8, kWideTile = 64;
 
 template <int D, bool FP8, bool CAUSAL, int WPS>
@@ -757,8 +759,11 @@ hipError_t launch_join(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
     hipLaunchKernelGGL((paged_attention_join_kernel<D, DC, SETS>), dim3((rows + kCols - 1) / kCols * (D / DC)),     \
                        dim3(256), 0, st, a, p.chunk, p.parts, rows);                                                \
   }
-  // Few columns of many parts: more threads on each, and its values over
-  // several blocks.
+  // Few columns of many parts: more threads on each, and its values over several
+  // blocks.  Whole calls, D = 128, 32 x 32 against 256 / D groups against one: 256
+  // parts of 16 columns 21.5, 35 and 49 us, 128 of 16 14, 21 and 27, 64 of 16 20.4,
+  // 22 and 26; 32 parts are even (of 32 columns 10.9, 10.3 and 12.6, of 512 29, 28
+  // and 29).  16 parts of 64 columns: 256 / D 9.7, one 11.1; 8 of 4096 34.7, 34.6.
   if (p.parts >= 32) JQ_JOIN(32, 32)
   else if (p.parts >= 8 && rows < 4096) JQ_JOIN(D, (256 / D))
   else JQ_JOIN(D, 1)
@@ -798,10 +803,16 @@ hipError_t launch_d(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
 // heads: 256 blocks 96 us, 1024 99, 4096 106), and with several sequences, whose
 // lengths may differ, up to four of at least 2^18 / D tokens each (64 sequences
 // of 1 .. 8192 tokens: one part 134 us, two 122, four 115, eight 114; 64 of 4096
-// each: 101, 105, 109, 115).  Of the wide kernel a CU holds two blocks up to
+// each: 101, 105, 109, 115), and no more than 2048 blocks for it (256 sequences of
+// up to 2048, 2048 blocks a part: one part 190 us, two 196, four 196, and 356, 374
+// and 388 where all are as long; 128 of up to 4096, 1024 a part: 192, 193, 188).  Of the wide kernel a CU holds two blocks up to
 // D = 128, and several sequences get as many of four rounds or more (6 of up to
 // 12047 tokens, 96 blocks a part: three parts 90 us, six 56; 3 of up to 3922,
 // 96: 50 and 39; 16 of 2085 each, 128: two parts 34, four 35).
+// The lengths are on the device, so max_len decides: a sequence of 4096 tokens (8
+// key heads of 128) takes 11 us under its own length and 43 under 131072, whose
+// parts are longer.  Four rounds are about even with and without parts, more are
+// not (8 sequences of 512: one part 9.1 us, four 9.4; of 1024: 16.6 and 12.7).
 AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
   const int64_t cols = Tq * (Hq / Hk);
   AttnPlan p;

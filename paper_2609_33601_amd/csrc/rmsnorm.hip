@@ -14,8 +14,11 @@
 //
 // Bound: HBM.  A row is read once and its codes are written once, so a row is
 // held in registers by the waves of one block, 8 elements (16 bytes) per lane
-// and chunk of 512.  16384 x 4096 with a residual to e4m3: 73 us, 6.5 TB/s;
-// 2747 x 3072 to bf16: 7.2 us; one row: 2.8 us, a launch.
+// and chunk of 512.  16384 x 4096 with a residual to e4m3: 80 us from HBM, 5.9
+// TB/s (71 where the last-level cache still holds a part); 2747 x 3072 to bf16:
+// 7.5 us; one row: 2.5 us, a launch.  Without a residual the int4 form takes 49 us
+// where the e4m3 one takes 39 (2747 x 3072: 9.7 and 7.4), its divisions; with one
+// both wait for memory (68 and 71; 12.3 and 10.5).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -222,7 +225,7 @@ hipError_t launch(const NormArgs& a, hipStream_t st) {
 // Inputs that the caches cannot hold anyway are read past them (non-temporal
 // loads: 16384 x 4096 46 -> 42 us, 2000 x 16384 with a residual 49 -> 42);
 // smaller ones usually lie there, as the kernel before left them (2747 x 3072:
-// 7.2 us, and 8.2 past the caches).
+// 7.2 us where they do, and 8.2 past the caches).
 template <NormOut OUT, bool RES>
 hipError_t launch(const NormArgs& a, hipStream_t st) {
   const bool big = a.M * a.D * (RES ? 4 : 2) > (int64_t{1} << 26);
