@@ -455,7 +455,7 @@ namespace {
 // 4096, weights from HBM) 0.8 and 17%.
 // 96 x 4096 -> 4096 takes 9.8 us with 48 x 32 blocks, 18 with 16 x 16 ones and 32
 // with 128 x 128; 1 x 4096 -> 4096 6.1 with 16 x 16 blocks and 13 with 64 x 64;
-// 4096 x 4096 -> 4096 68 with 256 x 256 and 85 with 128 x 128.
+// 4096 x 4096 -> 4096 68 with 256 x 256 and 90 with 128 x 128.
 struct Fp8Kernel {
   int mb, nb, waves, per_cu;            // of 16 rows and columns; waves that split K; blocks on a CU
   float launch, round, round_k, each_k;

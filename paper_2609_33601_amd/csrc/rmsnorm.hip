@@ -16,9 +16,9 @@
 // held in registers by the waves of one block, 8 elements (16 bytes) per lane
 // and chunk of 512.  16384 x 4096 with a residual to e4m3: 80 us from HBM, 5.9
 // TB/s (71 where the last-level cache still holds a part); 2747 x 3072 to bf16:
-// 7.5 us; one row: 2.5 us, a launch.  Without a residual the int4 form takes 49 us
-// where the e4m3 one takes 39 (2747 x 3072: 9.7 and 7.4), its divisions; with one
-// both wait for memory (68 and 71; 12.3 and 10.5).
+// 7.5 us; one row: 2.5 us, a launch.  16384 x 4096 without a residual takes the
+// int4 form 57 us and the e4m3 one 42 (a copy's rate: 32 and 38), for its
+// divisions; with a residual both wait for memory (78 and 82).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
