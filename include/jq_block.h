@@ -3,7 +3,10 @@
  * block's W4A4 linears (jq.h) when a model is served: the RMS norm that feeds
  * a quantised linear, an 8-bit linear for the layers that do not take 4 bits,
  * the rotation of new queries and keys with their append to a paged cache, and
- * the attention of the new tokens over that cache.
+ * the attention of the new tokens over that cache; and what whole prompts need
+ * besides: norms of each query and key head with their rotation, the gated
+ * activation, and attention of packed sequences of different lengths, over
+ * their own keys or over the cache.
  *
  * The conventions are those of jq.h: device pointers owned by the caller,
  * asynchronous on `stream`, nothing allocated, synchronised or printed,
@@ -187,6 +190,110 @@ jq_status jq_paged_attention(const void* q, const void* k_cache, const void* v_c
                              int64_t num_pages, int64_t page_size, int64_t max_len, float sm_scale, int causal,
                              jq_cache_type type, void* out, float* lse, void* workspace, size_t workspace_bytes,
                              void* stream);
+
+/*
+ * Norm of each head, rotation and append, in one pass: the queries and keys of T
+ * new tokens are first normalised over each head of D elements,
+ *     x <- (x * r) * weight,   r = 1 / sqrt(mean(x^2) + eps),
+ * then rotated as by jq_rope_append, in fp32 with one rounding at the end.
+ * Queries go to q_out; keys into the cache, or to k_out, or both (as bf16 in
+ * k_out, whatever the cache holds); values, unchanged, into the cache.
+ *   q_weight     in   [D] bf16 (NULL with Hq = 0)
+ *   k_weight     in   [D] bf16
+ *   k_out        out  [T,Hk,D] bf16, tokens k_out_stride apart, or NULL; it may be k itself
+ *   k_cache      NULL for a call without a cache: then v, slots, v_cache and the
+ *                     scales are NULL too, k_out is not, and num_pages, page_size
+ *                     and type are not looked at
+ * Everything else is as at jq_rope_append; a sum of squares past fp32's range
+ * makes r 0.  T * (Hq + 2 Hk) < 2^31; weights and k_out 16-byte aligned.
+ */
+jq_status jq_qk_norm_rope_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                 int64_t v_stride, int64_t T, int64_t Hq, int64_t Hk, int64_t D, const void* q_weight,
+                                 const void* k_weight, float eps, const int32_t* positions, const float* cos,
+                                 const float* sin, int64_t P, int64_t R, int interleaved, const int64_t* slots,
+                                 void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* k_cache,
+                                 void* v_cache, float* k_scale, float* v_scale, int64_t num_pages, int64_t page_size,
+                                 jq_cache_type type, void* stream);
+
+typedef enum {
+  JQ_ACT_SILU = 0,     /* x / (1 + e^-x) */
+  JQ_ACT_GELU = 1,     /* x Phi(x), Phi the normal distribution's */
+  JQ_ACT_GELU_TANH = 2 /* x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2 */
+} jq_act;
+
+/*
+ * The gated activation between two linears, y = act(gate) * up (act(gate) where
+ * up is NULL), in fp32 with one rounding at the end, written as jq_rmsnorm
+ * writes its y:
+ *   gate         in   [M,N] bf16, rows gate_stride elements apart
+ *   up           in   [M,N] bf16, rows up_stride apart, or NULL; gate and up may
+ *                     be the halves of one projection's rows
+ *   y            out  contiguous, by `out`: [M,N] bf16 or e4m3, or [M,N/2] packed int4
+ *   scale        out  fp32, [M, ceil(N/128)] for JQ_NORM_FP8, [M] for JQ_NORM_INT4; else NULL
+ * N % 8 == 0 (for JQ_NORM_INT4, N % 64 == 0), N <= 65536, M <= 2^30 and
+ * M * ceil(N/512) < 2^31; strides >= N and % 8 == 0; gate, up and y 16-byte aligned.
+ */
+jq_status jq_gated_act(const void* gate, int64_t gate_stride, const void* up, int64_t up_stride, int64_t M, int64_t N,
+                       jq_act act, jq_norm_out out, void* y, float* scale, void* stream);
+
+/* Bytes of workspace of jq_prompt_attention (0 where none is needed, and for invalid sizes). */
+size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int64_t Hq, int64_t Hk, int64_t D);
+
+/*
+ * Attention of packed sequences over their own keys and values, straight from
+ * the projections' rows (or what jq_qk_norm_rope_append wrote): sequence b has
+ * the rows starts[b] .. starts[b+1] of q and k_starts[b] .. k_starts[b+1] of k and v;
+ *     out = sum_t p_t v_t,  p = softmax over visible t of sm_scale * (q . k_t)
+ * For causal calls query i of n_q sees the keys t <= n_k - n_q + i of n_k (the last
+ * query sees the last key), else all of its sequence's.  A query that sees no
+ * key gives zeros, and lse = -inf.  Query head h reads key head h / (Hq / Hk).
+ *   q            in   [T,Hq,D] bf16, tokens q_stride elements apart
+ *   k, v         in   [Tk,Hk,D] bf16, tokens k_stride, v_stride apart
+ *   starts       in   [B+1] int32, not decreasing, within [0, T]
+ *   k_starts     in   [B+1] int32, not decreasing, within [0, Tk]; NULL: starts
+ *   out          out  [T,Hq,D] bf16
+ *   lse          out  [T,Hq] fp32 log of the softmax's denominator (natural
+ *                     logarithm, with the maximum in it), or NULL
+ *   workspace    at least jq_prompt_attention_workspace_bytes, 256-byte aligned
+ *                     (NULL where that is 0)
+ * Rows of out and lse before starts[0] and from starts[B] on stay as they are.
+ * Starts out of range count as the nearest in range and a sequence that would
+ * end before it begins as empty; where they decrease, what the rows hold is
+ * unspecified, and nothing outside the arrays is touched.
+ * An infinity or NaN among a token's values reaches the queries that see the
+ * token, and no other; a score of -infinity is a weight of 0.  The weights are
+ * rounded to bf16 for the product with the values; scores, statistics and sums are fp32.
+ * D = 64, 128 or 256; Hq % Hk == 0; T, Tk <= 2^30, B <= 2^20, T * Hq < 2^31 and
+ * fewer than 2^24 blocks (of 128 query columns of a key head and sequence);
+ * strides % 8 == 0, at least a token's elements, k_stride and v_stride <= 2^25.
+ */
+jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, const int32_t* starts, const int32_t* k_starts, int64_t T, int64_t Tk,
+                              int64_t B, int64_t Hq, int64_t Hk, int64_t D, float sm_scale, int causal, void* out,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of jq_chunk_attention (0 where none is needed, and for invalid sizes). */
+size_t jq_chunk_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len);
+
+/*
+ * The same over a paged cache: attention of chunks of new tokens, packed, of
+ * different lengths (single tokens among them), each over its sequence's
+ * cached tokens, the new ones (already appended) among them.  Sequence b has the
+ * rows starts[b] .. starts[b+1] of q and lens[b] cached tokens; for causal calls
+ * new token i of n sees the tokens t <= lens[b] - n + i.
+ *   q, starts, out, lse, workspace: as jq_prompt_attention
+ *   k_cache, v_cache, k_scale, v_scale, page_table, table_cols, lens, num_pages,
+ *   page_size, max_len, type: as jq_paged_attention, with B sequences
+ * A page number outside [0, num_pages) makes the outputs of the queries that see
+ * one of its tokens NaN, and may do so for others of its sequence.  For an 8-bit
+ * cache a weight is multiplied with its value's scale before it is rounded to bf16.
+ */
+jq_status jq_chunk_attention(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                             const float* k_scale, const float* v_scale, const int32_t* page_table, int64_t table_cols,
+                             const int32_t* starts, const int32_t* lens, int64_t T, int64_t B, int64_t Hq, int64_t Hk,
+                             int64_t D, int64_t num_pages, int64_t page_size, int64_t max_len, float sm_scale,
+                             int causal, jq_cache_type type, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

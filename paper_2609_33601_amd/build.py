@@ -25,7 +25,8 @@ OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libjq.so")
 SOURCES = ["quantize.hip", "ternary.hip", "gemm.hip", "gemm_narrow.hip", "gemm_wide.hip", "gemm_group.hip", "f6.hip",
            "f6_narrow.hip", "f6_narrow_group.hip", "f6_quant_few.hip", "jq_api.cpp", "rmsnorm.hip", "fp8_quant.hip",
-           "fp8_gemm.hip", "rope_append.hip", "paged_attention.hip", "jq_block_api.cpp"]
+           "fp8_gemm.hip", "rope_append.hip", "paged_attention.hip", "gated_act.hip", "prompt_attention.hip",
+           "jq_block_api.cpp"]
 # The compiled half of the binding of jq_block.h: a Python extension on torch's C++ headers.
 BINDING_SOURCE = "jq_block_py.cpp"
 BINDING = os.path.join(PKG, "_jq_block.so")
@@ -38,7 +39,7 @@ SOURCE_FLAGS = {"f6.hip": ["-mllvm", "-disable-machine-sink"], "fp8_gemm.hip": [
 # Sources whose asm-issued loads are checked against their waits, and the
 # kernel names checked in each.
 CHECKED_SOURCES = {"f6.hip": "w4a4_f6_gemm_kernel", "fp8_gemm.hip": "fp8_gemm_kernel",
-                   "paged_attention.hip": "paged_attention_wide_kernel"}
+                   "paged_attention.hip": "paged_attention_wide_kernel", "prompt_attention.hip": "prompt_attention_kernel"}
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}",

@@ -80,6 +80,18 @@ __device__ __forceinline__ float e4m3_quotient(float v, E4m3Divisor d) {
   return fmaf(fmaf(-q, d.s, v), d.inv, q);
 }
 
+// Eight int4 codes, clamp(rne(y / s), -8, 7), by one division each.
+__device__ __forceinline__ uint32_t int4_codes(const float* y, float s) {
+  uint32_t out = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float t = s == 0.0f ? 0.0f : __builtin_rintf(y[j] / s);
+    t = fminf(fmaxf(t, -8.0f), 7.0f);
+    out |= (static_cast<uint32_t>(static_cast<int>(t)) & 0xFu) << (4 * j);
+  }
+  return out;
+}
+
 // The value of another lane of the same row of 16 (DPP), all lanes taking part.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {

@@ -25,6 +25,16 @@ struct NormArgs {
 constexpr int64_t kNormMaxD = 65536;
 hipError_t launch_rmsnorm(const NormArgs& a, NormOut out, hipStream_t st);
 
+enum class Act { kSilu = 0, kGelu = 1, kGeluTanh = 2 };
+struct ActArgs {
+  const uint16_t *gate, *up;         // up: nullptr for act(gate) alone
+  void* y;
+  float* scale;
+  int64_t M, gate_stride, up_stride;  // elements between rows
+  int N;
+};
+hipError_t launch_gated_act(const ActArgs& a, Act act, NormOut out, hipStream_t st);
+
 // bf16 [M,K] (rows x_stride apart) -> e4m3 codes [M,K] and scales [M, ceil(K/128)].
 hipError_t launch_quantize_fp8(const uint16_t* x, int64_t x_stride, int64_t M, int64_t K, uint8_t* q, float* scale,
                                hipStream_t st);
@@ -49,8 +59,15 @@ struct AppendArgs {
   int64_t T, P, num_slots;
   int Hq, Hk, D, R, page, page_shift;
   bool interleaved, fp8;
+  // with a norm of each head first, and then also with the keys written
+  // densely, and without a cache (k_cache = nullptr)
+  const uint16_t *q_weight = nullptr, *k_weight = nullptr;
+  float eps = 0.0f;
+  uint16_t* k_out = nullptr;
+  int64_t k_out_stride = 0;
 };
 hipError_t launch_rope_append(const AppendArgs& a, hipStream_t st);
+hipError_t launch_norm_rope_append(const AppendArgs& a, hipStream_t st);
 
 struct AttnArgs {
   const uint16_t* q;  // [B, Tq, Hq, D]
@@ -74,6 +91,32 @@ struct AttnPlan {
 };
 AttnPlan attention_plan(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len);
 hipError_t launch_paged_attention(const AttnArgs& a, hipStream_t st);
+
+// Attention of packed new tokens: over packed keys and values of their own, or over a paged cache.
+enum class PromptKv { kDense, kPagedBf16, kPagedFp8 };
+struct PromptArgs {
+  const uint16_t* q;  // [T, Hq, D], tokens q_stride elements apart
+  const void *k, *v;  // dense: [Tk, Hk, D] bf16, tokens k_stride, v_stride elements apart; else the cache
+  const float *k_scale, *v_scale;
+  const int32_t *starts, *k_starts;  // [B + 1]; k_starts: dense only
+  const int32_t *table, *lens;       // paged only: [B, table_cols], [B]
+  uint16_t* out;                     // [T, Hq, D]
+  float* lse;                        // [T, Hq] or nullptr
+  float* ws;
+  int64_t T, Tk, q_stride, k_stride, v_stride, num_pages;
+  int B, Hq, Hk, D, page_shift, table_cols, max_len;
+  float scale;
+  bool causal;
+  PromptKv kv;
+};
+// How a call is cut: columns (new tokens times heads that share a key head) of
+// a tile, the most tiles that the sequences can have, keys of a part, parts.
+struct PromptPlan {
+  int cols, parts;
+  int64_t tiles, chunk;
+};
+PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len);
+hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t st);
 
 }  // namespace jq
 

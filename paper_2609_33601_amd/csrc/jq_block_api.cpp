@@ -108,6 +108,50 @@ size_t attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, 
   return round_up(rows * (static_cast<size_t>(D) + 2) * sizeof(float), kWsAlign);
 }
 
+// Sizes of jq_prompt_attention and jq_chunk_attention.
+jq_status check_prompt(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
+  if (T <= 0 || B <= 0 || Hq <= 0 || Hk <= 0 || max_len <= 0) return JQ_ERR_INVALID_ARG;
+  if (Hq % Hk != 0 || (D != 64 && D != 128 && D != 256)) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (T > kMaxAxis || max_len > kMaxAxis || B > (1 << 20) || Hq > 65536) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (T * Hq >= (int64_t(1) << 31)) return JQ_ERR_UNSUPPORTED_SHAPE;
+  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len);
+  // grids of fewer than 2^24 blocks of 256 threads
+  return p.tiles * Hk * p.parts < kMaxBlocks ? JQ_OK : JQ_ERR_UNSUPPORTED_SHAPE;
+}
+
+size_t prompt_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
+  if (check_prompt(T, B, Hq, Hk, D, max_len) != JQ_OK) return 0;
+  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len);
+  if (p.parts == 1) return 0;
+  const size_t rows = static_cast<size_t>(T) * static_cast<size_t>(Hq) * p.parts;
+  return round_up(rows * (static_cast<size_t>(D) + 2) * sizeof(float), kWsAlign);
+}
+
+// What the two calls share: the queries, their starts, outputs and workspace.
+jq_status check_prompt_call(const void* q, int64_t q_stride, const int32_t* starts, int64_t T, int64_t B, int64_t Hq,
+                            int64_t Hk, int64_t D, int64_t max_len, const void* out, const float* lse,
+                            const void* workspace, size_t workspace_bytes) {
+  if (q == nullptr || starts == nullptr || out == nullptr) return JQ_ERR_INVALID_ARG;
+  jq_status st = check_prompt(T, B, Hq, Hk, D, max_len);
+  if (st == JQ_OK) st = check_stride(q_stride, Hq * D);
+  if (st != JQ_OK) return st;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(starts, 4) || !aligned(lse, 4)) return JQ_ERR_MISALIGNED;
+  const size_t need = prompt_workspace_bytes(T, B, Hq, Hk, D, max_len);
+  if (need > 0) {
+    if (workspace == nullptr) return JQ_ERR_INVALID_ARG;
+    if (!aligned(workspace, kWsAlign)) return JQ_ERR_MISALIGNED;
+    if (workspace_bytes < need) return JQ_ERR_WORKSPACE_TOO_SMALL;
+  }
+  return JQ_OK;
+}
+
+// Sixteen rows of keys (or values) are one descriptor, whose offsets have 31 bits.
+constexpr int64_t kMaxKeyStride = int64_t(1) << 25;
+jq_status check_key_stride(int64_t stride, int64_t width) {
+  const jq_status st = check_stride(stride, width);
+  return st == JQ_OK && stride > kMaxKeyStride ? JQ_ERR_INVALID_ARG : st;
+}
+
 }  // namespace
 
 extern "C" {
@@ -209,7 +253,7 @@ jq_status jq_rope_append(const void* q, int64_t q_stride, const void* k, int64_t
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || !aligned(cos, 16) ||
       !aligned(sin, 16) || !aligned(positions, 4) || !aligned(slots, 8))
     return JQ_ERR_MISALIGNED;
-  jq::AppendArgs a;
+  jq::AppendArgs a = {};
   a.q = u16(q), a.k = u16(k), a.v = u16(v), a.q_out = static_cast<uint16_t*>(q_out);
   a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
   a.positions = positions, a.cos = cos, a.sin = sin, a.slots = slots;
@@ -255,6 +299,125 @@ jq_status jq_paged_attention(const void* q, const void* k_cache, const void* v_c
   a.D = static_cast<int>(D), a.page_shift = page_shift(page_size), a.table_cols = static_cast<int>(table_cols);
   a.max_len = static_cast<int>(max_len), a.scale = sm_scale, a.causal = causal != 0, a.fp8 = type == JQ_CACHE_FP8;
   return from_hip(jq::launch_paged_attention(a, as_stream(stream)));
+}
+
+jq_status jq_qk_norm_rope_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                 int64_t v_stride, int64_t T, int64_t Hq, int64_t Hk, int64_t D, const void* q_weight,
+                                 const void* k_weight, float eps, const int32_t* positions, const float* cos,
+                                 const float* sin, int64_t P, int64_t R, int interleaved, const int64_t* slots,
+                                 void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* k_cache,
+                                 void* v_cache, float* k_scale, float* v_scale, int64_t num_pages, int64_t page_size,
+                                 jq_cache_type type, void* stream) {
+  const bool cached = k_cache != nullptr;
+  if (k == nullptr || positions == nullptr || k_weight == nullptr) return JQ_ERR_INVALID_ARG;
+  if (cached != (v != nullptr) || cached != (slots != nullptr) || cached != (v_cache != nullptr)) return JQ_ERR_INVALID_ARG;
+  if (!cached && (k_out == nullptr || k_scale != nullptr || v_scale != nullptr)) return JQ_ERR_INVALID_ARG;
+  if (T <= 0 || D <= 0 || Hk <= 0 || Hq < 0 || R < 0 || P < 0) return JQ_ERR_INVALID_ARG;
+  if ((Hq > 0) != (q != nullptr) || (Hq > 0) != (q_out != nullptr) || (Hq > 0) != (q_weight != nullptr))
+    return JQ_ERR_INVALID_ARG;
+  if (R > 0 && (cos == nullptr || sin == nullptr || P == 0)) return JQ_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f)) return JQ_ERR_INVALID_ARG;
+  jq_status st = cached ? check_cache(Hk, k_cache, v_cache, k_scale, v_scale, num_pages, page_size, type) : JQ_OK;
+  if (st != JQ_OK) return st;
+  if (D % 16 != 0 || D > 256 || R % 16 != 0 || R > D || Hq > 65536 || Hk > 65536) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (T > kMaxRows || T * (Hq + 2 * Hk) >= (int64_t(1) << 31)) return JQ_ERR_UNSUPPORTED_SHAPE;
+  st = check_stride(k_stride, Hk * D);
+  if (st == JQ_OK && cached) st = check_stride(v_stride, Hk * D);
+  if (st == JQ_OK && Hq > 0) st = check_stride(q_stride, Hq * D);
+  if (st == JQ_OK && Hq > 0) st = check_stride(q_out_stride, Hq * D);
+  if (st == JQ_OK && k_out != nullptr) st = check_stride(k_out_stride, Hk * D);
+  if (st != JQ_OK) return st;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) ||
+      !aligned(q_weight, 16) || !aligned(k_weight, 16) || !aligned(cos, 16) || !aligned(sin, 16) ||
+      !aligned(positions, 4) || !aligned(slots, 8))
+    return JQ_ERR_MISALIGNED;
+  jq::AppendArgs a = {};
+  a.q = u16(q), a.k = u16(k), a.v = u16(v), a.q_out = static_cast<uint16_t*>(q_out);
+  a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
+  a.positions = positions, a.cos = cos, a.sin = sin, a.slots = slots;
+  a.T = T, a.P = P;
+  a.Hq = static_cast<int>(Hq), a.Hk = static_cast<int>(Hk), a.D = static_cast<int>(D), a.R = static_cast<int>(R);
+  a.interleaved = interleaved != 0;
+  if (cached) {
+    a.k_cache = k_cache, a.v_cache = v_cache, a.k_scale = k_scale, a.v_scale = v_scale;
+    a.num_slots = num_pages * page_size;
+    a.page = static_cast<int>(page_size), a.page_shift = page_shift(page_size);
+    a.fp8 = type == JQ_CACHE_FP8;
+  }
+  a.q_weight = u16(q_weight), a.k_weight = u16(k_weight), a.eps = eps;
+  a.k_out = static_cast<uint16_t*>(k_out), a.k_out_stride = k_out_stride;
+  return from_hip(jq::launch_norm_rope_append(a, as_stream(stream)));
+}
+
+jq_status jq_gated_act(const void* gate, int64_t gate_stride, const void* up, int64_t up_stride, int64_t M, int64_t N,
+                       jq_act act, jq_norm_out out, void* y, float* scale, void* stream) {
+  if (gate == nullptr || y == nullptr || M <= 0 || N <= 0) return JQ_ERR_INVALID_ARG;
+  if (act != JQ_ACT_SILU && act != JQ_ACT_GELU && act != JQ_ACT_GELU_TANH) return JQ_ERR_INVALID_ARG;
+  if (out != JQ_NORM_BF16 && out != JQ_NORM_FP8 && out != JQ_NORM_INT4) return JQ_ERR_INVALID_ARG;
+  if ((out != JQ_NORM_BF16) != (scale != nullptr)) return JQ_ERR_INVALID_ARG;
+  if (M > kMaxRows || N % 8 != 0 || N > kMaxK) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (out == JQ_NORM_INT4 && N % 64 != 0) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (M * ((N + 511) / 512) >= (int64_t(1) << 31)) return JQ_ERR_UNSUPPORTED_SHAPE;
+  jq_status st = check_stride(gate_stride, N);
+  if (st == JQ_OK && up != nullptr) st = check_stride(up_stride, N);
+  if (st != JQ_OK) return st;
+  if (!aligned(gate, 16) || !aligned(up, 16) || !aligned(y, 16) || !aligned(scale, 4)) return JQ_ERR_MISALIGNED;
+  jq::ActArgs a;
+  a.gate = u16(gate), a.up = u16(up), a.y = y, a.scale = scale;
+  a.M = M, a.gate_stride = gate_stride, a.up_stride = up_stride, a.N = static_cast<int>(N);
+  return from_hip(jq::launch_gated_act(a, static_cast<jq::Act>(act), static_cast<jq::NormOut>(out), as_stream(stream)));
+}
+
+size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int64_t Hq, int64_t Hk, int64_t D) {
+  return prompt_workspace_bytes(T, B, Hq, Hk, D, Tk);
+}
+
+jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, const int32_t* starts, const int32_t* k_starts, int64_t T, int64_t Tk,
+                              int64_t B, int64_t Hq, int64_t Hk, int64_t D, float sm_scale, int causal, void* out,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (k == nullptr || v == nullptr) return JQ_ERR_INVALID_ARG;
+  jq_status st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, Tk, out, lse, workspace, workspace_bytes);
+  if (st == JQ_OK) st = check_key_stride(k_stride, Hk * D);
+  if (st == JQ_OK) st = check_key_stride(v_stride, Hk * D);
+  if (st != JQ_OK) return st;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_starts, 4)) return JQ_ERR_MISALIGNED;
+  jq::PromptArgs a = {};
+  a.q = u16(q), a.k = k, a.v = v, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.starts = starts, a.k_starts = k_starts != nullptr ? k_starts : starts;
+  a.out = static_cast<uint16_t*>(out), a.lse = lse, a.ws = static_cast<float*>(workspace);
+  a.T = T, a.Tk = Tk, a.B = static_cast<int>(B), a.Hq = static_cast<int>(Hq), a.Hk = static_cast<int>(Hk);
+  a.D = static_cast<int>(D), a.max_len = static_cast<int>(Tk), a.scale = sm_scale, a.causal = causal != 0;
+  a.kv = jq::PromptKv::kDense;
+  return from_hip(jq::launch_prompt_attention(a, as_stream(stream)));
+}
+
+size_t jq_chunk_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
+  return prompt_workspace_bytes(T, B, Hq, Hk, D, max_len);
+}
+
+jq_status jq_chunk_attention(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                             const float* k_scale, const float* v_scale, const int32_t* page_table, int64_t table_cols,
+                             const int32_t* starts, const int32_t* lens, int64_t T, int64_t B, int64_t Hq, int64_t Hk,
+                             int64_t D, int64_t num_pages, int64_t page_size, int64_t max_len, float sm_scale,
+                             int causal, jq_cache_type type, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  if (page_table == nullptr || lens == nullptr || table_cols <= 0) return JQ_ERR_INVALID_ARG;
+  jq_status st = check_cache(Hk, k_cache, v_cache, k_scale, v_scale, num_pages, page_size, type);
+  if (st == JQ_OK) st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, max_len, out, lse, workspace, workspace_bytes);
+  if (st != JQ_OK) return st;
+  if (table_cols > kMaxAxis) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (max_len > table_cols * page_size) return JQ_ERR_INVALID_ARG;
+  if (!aligned(page_table, 4) || !aligned(lens, 4)) return JQ_ERR_MISALIGNED;
+  jq::PromptArgs a = {};
+  a.q = u16(q), a.k = k_cache, a.v = v_cache, a.q_stride = q_stride, a.k_scale = k_scale, a.v_scale = v_scale;
+  a.starts = starts, a.table = page_table, a.lens = lens, a.table_cols = static_cast<int>(table_cols);
+  a.out = static_cast<uint16_t*>(out), a.lse = lse, a.ws = static_cast<float*>(workspace), a.num_pages = num_pages;
+  a.T = T, a.B = static_cast<int>(B), a.Hq = static_cast<int>(Hq), a.Hk = static_cast<int>(Hk);
+  a.D = static_cast<int>(D), a.page_shift = page_shift(page_size), a.max_len = static_cast<int>(max_len);
+  a.scale = sm_scale, a.causal = causal != 0;
+  a.kv = type == JQ_CACHE_FP8 ? jq::PromptKv::kPagedFp8 : jq::PromptKv::kPagedBf16;
+  return from_hip(jq::launch_prompt_attention(a, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -355,6 +355,175 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// q, k, v, q_weight, k_weight, positions, cos, sin, slots, k_cache, v_cache, k_scale, v_scale, eps, interleaved,
+// dense_k, q_out, k_out, stream; the rotated q and k (None: not returned)
+PyObject* qk_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  count(n, 19);
+  const bool cached = a[9] != Py_None;
+  const at::ScalarType type = cached ? cache_type(a[9], a[11], a[12]) : kBf16;
+  Call c(a[1], "k", a[18]);
+  const Tensor& k = c.tensor(a[1], "k", kBf16);
+  TORCH_CHECK_VALUE(k.dim() == 3, "k must be [T, Hk, D], got shape ", k.sizes());
+  const int64_t T = k.size(0), Hk = k.size(1), D = k.size(2);
+  int64_t ks = 0, vs = 0, qs = 0, qos = 0, kos = 0, Hq = 0, P = 0, R = 0;
+  c.rows(a[1], "k", k.sizes(), &ks);
+  std::optional<Cache> kv;
+  const void* vp = nullptr;
+  const int64_t* slots = nullptr;
+  if (cached) {
+    kv.emplace(cache(c, type, a[9], a[10], a[11], a[12]));
+    TORCH_CHECK_VALUE(kv->Hk == Hk && kv->D == D, "k has ", Hk, " heads of ", D, ", the cache ", kv->Hk, " of ", kv->D);
+    vp = ptr(c.rows(a[2], "v", k.sizes(), &vs));
+    slots = static_cast<const int64_t*>(ptr(c.dense(a[8], "slots", at::kLong, {T})));
+  } else {
+    TORCH_CHECK_VALUE(a[8] == Py_None && a[10] == Py_None && a[11] == Py_None && a[12] == Py_None,
+                      "slots, v_cache or scales without a k_cache");
+  }
+  const void *qp = nullptr, *qw = nullptr;
+  Tensor q_out, k_out;
+  if (a[0] != Py_None) {
+    const Tensor& q = c.tensor(a[0], "q", kBf16);
+    TORCH_CHECK_VALUE(q.dim() == 3 && q.size(1) > 0, "q must be [T, Hq, D], got shape ", q.sizes());
+    Hq = q.size(1);
+    qp = ptr(c.rows(a[0], "q", {T, Hq, D}, &qs));
+    qw = ptr(c.dense(a[3], "q_weight", kBf16, {D}));
+    q_out = a[16] == Py_None ? c.make(kBf16, {T, Hq, D}) : c.rows(a[16], "q_out", {T, Hq, D}, &qos);
+    if (a[16] == Py_None) qos = Hq * D;
+  } else {
+    TORCH_CHECK_VALUE(a[16] == Py_None, "q_out without q");
+  }
+  const Tensor& kw = c.dense(a[4], "k_weight", kBf16, {D});
+  if (a[17] != Py_None) {
+    k_out = c.rows(a[17], "k_out", k.sizes(), &kos);
+  } else if (!cached || truth(a[15])) {
+    k_out = c.make(kBf16, k.sizes());
+    kos = Hk * D;
+  }
+  const float *cos = nullptr, *sin = nullptr;
+  if (a[6] != Py_None) {
+    const Tensor& t = matrix(c.dense(a[6], "cos", kF32), "cos");
+    P = t.size(0), R = 2 * t.size(1);
+    cos = f32(t), sin = f32(c.dense(a[7], "sin", kF32, t.sizes()));
+  } else {
+    TORCH_CHECK_VALUE(a[7] == Py_None, "sin without cos");
+  }
+  const Tensor& pos = c.dense(a[5], "positions", at::kInt, {T});
+  const jq_status st = jq_qk_norm_rope_append(
+      qp, qs, ptr(k), ks, vp, vs, T, Hq, Hk, D, qw, ptr(kw), static_cast<float>(number(a[13])),
+      static_cast<const int32_t*>(ptr(pos)), cos, sin, P, R, truth(a[14]), slots, q_out.defined() ? ptr(q_out) : nullptr,
+      qos, k_out.defined() ? ptr(k_out) : nullptr, kos, kv ? ptr(kv->k) : nullptr, kv ? ptr(kv->v) : nullptr,
+      kv ? kv->ks : nullptr, kv ? kv->vs : nullptr, kv ? kv->pages : 0, kv ? kv->page : 0,
+      kv ? kv->type : JQ_CACHE_BF16, c.stream());
+  if (st != JQ_OK) return refused(st);
+  PyObject* r = PyTuple_New(2);
+  if (r == nullptr) throw python_error();
+  auto item = [](const Tensor& t) { return t.defined() ? wrap(t) : Py_NewRef(Py_None); };
+  PyTuple_SET_ITEM(r, 0, item(q_out));
+  PyTuple_SET_ITEM(r, 1, item(k_out));
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
+// gate, up, act, out, y, scale, stream
+PyObject* gated_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  count(n, 7);
+  Call c(a[0], "gate", a[6]);
+  const Tensor& gate = matrix(c.tensor(a[0], "gate", kBf16), "gate");
+  const int64_t M = gate.size(0), N = gate.size(1), out = integer(a[3]);
+  int64_t gs = 0, us = 0;
+  c.rows(a[0], "gate", gate.sizes(), &gs);
+  const void* up = a[1] == Py_None ? nullptr : ptr(c.rows(a[1], "up", gate.sizes(), &us));
+  Tensor y = c.out(a[4], "y", out == JQ_NORM_BF16 ? kBf16 : out == JQ_NORM_FP8 ? kFp8 : at::kByte,
+                   {M, out == JQ_NORM_INT4 ? N / 2 : N});
+  Tensor scale;
+  if (out == JQ_NORM_FP8) scale = c.out(a[5], "scale", kF32, {M, blocks(N)});
+  else if (out == JQ_NORM_INT4) scale = c.out(a[5], "scale", kF32, {M});
+  else TORCH_CHECK_VALUE(a[5] == Py_None, "a bf16 output has no scale");
+  const jq_status st = jq_gated_act(ptr(gate), gs, up, us, M, N, static_cast<jq_act>(integer(a[2])),
+                                    static_cast<jq_norm_out>(out), ptr(y), scale.defined() ? f32(scale) : nullptr,
+                                    c.stream());
+  if (st != JQ_OK) return refused(st);
+  if (scale.defined()) return wrap(y, scale);
+  PyObject* r = PyTuple_New(1);
+  if (r == nullptr) throw python_error();
+  PyTuple_SET_ITEM(r, 0, wrap(y));
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
+// The packed queries of the two calls below, with their starts.
+struct Packed {
+  const Tensor& q;
+  const Tensor& starts;
+  int64_t T, B, Hq, D, stride;
+};
+Packed packed(const Call& c, PyObject* qo, PyObject* so) {
+  const Tensor& q = c.tensor(qo, "q", kBf16);
+  TORCH_CHECK_VALUE(q.dim() == 3, "q must be [T, Hq, D], got shape ", q.sizes());
+  int64_t stride = 0;
+  c.rows(qo, "q", q.sizes(), &stride);
+  const Tensor& s = c.dense(so, "starts", at::kInt);
+  TORCH_CHECK_VALUE(s.dim() == 1 && s.size(0) >= 2, "starts must be [B + 1], got shape ", s.sizes());
+  return {q, s, q.size(0), s.size(0) - 1, q.size(1), q.size(2), stride};
+}
+Tensor workspace(const Call& c, PyObject* o, size_t need) {
+  if (o != Py_None) return c.dense(o, "workspace", at::kByte);
+  return need ? c.make(at::kByte, {static_cast<int64_t>(need)}) : Tensor();
+}
+double sm_scale(PyObject* o, int64_t D) { return o == Py_None ? 1.0 / std::sqrt(static_cast<double>(D)) : number(o); }
+const int32_t* i32(const Tensor& t) { return static_cast<const int32_t*>(ptr(t)); }
+
+// q, k, v, starts, k_starts, causal, sm_scale, out, lse, workspace, stream
+PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  count(n, 11);
+  Call c(a[0], "q", a[10]);
+  const Packed p = packed(c, a[0], a[3]);
+  const Tensor& k = c.tensor(a[1], "k", kBf16);
+  TORCH_CHECK_VALUE(k.dim() == 3 && k.size(2) == p.D, "k must be [Tk, Hk, ", p.D, "], got shape ", k.sizes());
+  const int64_t Tk = k.size(0), Hk = k.size(1);
+  int64_t ks = 0, vs = 0;
+  c.rows(a[1], "k", k.sizes(), &ks);
+  const Tensor& v = c.rows(a[2], "v", k.sizes(), &vs);
+  TORCH_CHECK_VALUE(a[4] != Py_None || Tk == p.T, "without k_starts k must have the ", p.T, " tokens of q, got ", Tk);
+  const int32_t* k_starts = a[4] == Py_None ? nullptr : i32(c.dense(a[4], "k_starts", at::kInt, {p.B + 1}));
+  Tensor out = c.out(a[7], "out", kBf16, p.q.sizes());
+  float* lse = a[8] == Py_None ? nullptr : f32(c.dense(a[8], "lse", kF32, {p.T, p.Hq}));
+  const Tensor ws = workspace(c, a[9], jq_prompt_attention_workspace_bytes(p.T, Tk, p.B, p.Hq, Hk, p.D));
+  const jq_status st = jq_prompt_attention(
+      ptr(p.q), p.stride, ptr(k), ks, ptr(v), vs, i32(p.starts), k_starts, p.T, Tk, p.B, p.Hq, Hk, p.D,
+      static_cast<float>(sm_scale(a[6], p.D)), truth(a[5]), ptr(out), lse, ws.defined() ? ptr(ws) : nullptr,
+      ws.defined() ? ws.numel() : 0, c.stream());
+  return st == JQ_OK ? wrap(out) : refused(st);
+  END_HANDLE_TH_ERRORS
+}
+
+// q, k_cache, v_cache, page_table, starts, lens, k_scale, v_scale, max_len, sm_scale, causal, out, lse, workspace, stream
+PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  count(n, 15);
+  const at::ScalarType type = cache_type(a[1], a[6], a[7]);
+  Call c(a[0], "q", a[14]);
+  const Cache kv = cache(c, type, a[1], a[2], a[6], a[7]);
+  const Packed p = packed(c, a[0], a[4]);
+  TORCH_CHECK_VALUE(p.D == kv.D, "q has heads of ", p.D, ", the cache of ", kv.D);
+  const Tensor& table = c.dense(a[3], "page_table", at::kInt);
+  TORCH_CHECK_VALUE(table.dim() == 2 && table.size(0) == p.B, "page_table must be [", p.B, ", columns], got shape ", table.sizes());
+  const Tensor& lens = c.dense(a[5], "lens", at::kInt, {p.B});
+  const int64_t max_len = a[8] == Py_None ? table.size(1) * kv.page : integer(a[8]);
+  Tensor out = c.out(a[11], "out", kBf16, p.q.sizes());
+  float* lse = a[12] == Py_None ? nullptr : f32(c.dense(a[12], "lse", kF32, {p.T, p.Hq}));
+  const Tensor ws = workspace(c, a[13], jq_chunk_attention_workspace_bytes(p.T, p.B, p.Hq, kv.Hk, p.D, max_len));
+  const jq_status st = jq_chunk_attention(
+      ptr(p.q), p.stride, ptr(kv.k), ptr(kv.v), kv.ks, kv.vs, i32(table), table.size(1), i32(p.starts), i32(lens), p.T,
+      p.B, p.Hq, kv.Hk, p.D, kv.pages, kv.page, max_len, static_cast<float>(sm_scale(a[9], p.D)), truth(a[10]), kv.type,
+      ptr(out), lse, ws.defined() ? ptr(ws) : nullptr, ws.defined() ? ws.numel() : 0, c.stream());
+  return st == JQ_OK ? wrap(out) : refused(st);
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -367,6 +536,10 @@ PyMethodDef methods[] = {method<rmsnorm>("rmsnorm"),
                          method<fp8_linear>("fp8_linear"),
                          method<rope_append>("rope_append"),
                          method<paged_attention>("paged_attention"),
+                         method<qk_norm_rope_append>("qk_norm_rope_append"),
+                         method<gated_act>("gated_act"),
+                         method<prompt_attention>("prompt_attention"),
+                         method<chunk_attention>("chunk_attention"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_jq_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,650 @@
+// Attention of many new tokens for gfx950: packed prompts of different lengths
+// over their own keys and values, or chunks of new tokens, packed too, over a
+// paged cache.
+//
+//   p = softmax over visible t of scale * (q . k_t),  o = sum_t p_t v_t
+//   visible: t < n_k, and for causal calls t <= n_k - n_q + i for new token i.
+//   A query that sees nothing gives zeros (and lse = -inf).
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "block_common.h"
+#include "block_internal.h"
+
+namespace jq {
+
+namespace {
+
+using namespace block_detail;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef const __attribute__((address_space(4))) int32_t* uniform_i32;
+typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4;
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ float max_halves(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// What a product is multiplied with to be a power of two; 0 as next to nothing,
+// for the masked ones' sake.
+__device__ __forceinline__ float power_scale(float scale) {
+  return scale == 0.0f ? 0x1p-126f : fabsf(scale) * 1.44269504088896340736f;
+}
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
+// A block's place: a sequence, its rows in the packed tensors and its tile of columns.
+struct Place {
+  int seq, row0, rows, tile;
+};
+
+// The `index`-th tile of `per` columns, counted from the last one of the last
+// sequence, so that the longest of a causal sequence come first.  All lanes of
+// a wave take part, 64 sequences at a time; seq = -1 where there are fewer
+// tiles.  Starts outside [0, T] are brought into it, so whatever they are, the
+// rows lie in the tensors.
+__device__ __forceinline__ void rows_of(const int32_t* starts, int64_t T, int b, int* row0, int* rows) {
+  const int t = static_cast<int>(T);
+  const int s0 = min(max(starts[b], 0), t), s1 = min(max(starts[b + 1], 0), t);
+  *row0 = s0;
+  *rows = max(s1 - s0, 0);
+}
+__device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, int index) {
+  const int lane = threadIdx.x & 63;
+  auto tiles_of = [&](int b, int* row0, int* rows) {
+    *row0 = *rows = 0;
+    if (b < a.B) rows_of(a.starts, a.T, b, row0, rows);
+    return (*rows * G + per - 1) / per;
+  };
+  Place p{-1, 0, 0, 0};
+  int after = 0;  // tiles of the sequences behind
+  for (int base = (a.B - 1) / 64 * 64; base >= 0; base -= 64) {
+    int row0, rows;
+    const int n = tiles_of(base + lane, &row0, &rows);
+    int upto = n;  // tiles of this lane's sequence and those behind it, of these 64
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int v = __shfl_down(upto, d, 64);
+      upto += lane + d < 64 ? v : 0;
+    }
+    const int mine = index - after - (upto - n);  // place among this sequence's tiles, from its last
+    const uint64_t hit = __ballot(mine >= 0 && mine < n);
+    if (hit != 0) {
+      const int l = __builtin_ctzll(hit);
+      p.seq = base + l;
+      p.row0 = __builtin_amdgcn_readlane(row0, l);
+      p.rows = __builtin_amdgcn_readlane(rows, l);
+      p.tile = __builtin_amdgcn_readlane(n - 1 - mine, l);
+      return p;
+    }
+    after += __builtin_amdgcn_readlane(upto, 0);
+  }
+  return p;
+}
+
+// Which 16-byte chunk of a row in LDS holds chunk c.  Keys are read a row a
+// lane, 16 bytes each; values transposed, 64 bytes of each of eight rows: both
+// touch every bank evenly this way.
+template <int D>
+__device__ __forceinline__ int key_slot(int row, int c) {
+  constexpr int kMask = D / 8 < 16 ? D / 8 - 1 : 15;
+  return c ^ (row & kMask);
+}
+template <int D>
+__device__ __forceinline__ int value_slot(int row, int c) {
+  return D == 64 ? c ^ ((row >> 1 & 1) << 2) : c ^ ((row & 3) << 2);
+}
+
+template <int D, int QG, PromptKv KV>
+struct Sizes {
+  static constexpr int kKeys = D == 256 ? 32 : 64;  // keys of a step
+  static constexpr int kRow = 2 * D;                // bytes of a row in LDS
+  static constexpr int kHalf = kKeys * kRow;        // a step's keys, or its values
+  static constexpr int kStage = 2 * kHalf + (KV == PromptKv::kPagedFp8 ? 8 * kKeys : 0);
+  static constexpr int kCols = 4 * 32 * QG;         // columns of a block
+  static constexpr int kPerSimd = D == 64 || (D == 128 && QG == 1) ? 2 : 1;
+};
+
+// One column's keys [t0, t1) by one wave, in fp32 and straight from memory: for
+// columns beside which a product met an infinity or NaN among the values of
+// tokens that only some of its columns see (such a value times a weight of 0
+// would count).  A lane takes a key at a time for the scores and D / 64 values
+// of the output.  Nothing of the fast path is alive here, so it costs that path
+// no registers (masks inside its product took 70 more).
+template <int D, PromptKv KV>
+__device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int token, int head, int hk, int key0, int t0, int t1,
+                                        int part, int parts, bool bad) {
+  constexpr int kPer = D / 64;
+  const int lane = threadIdx.x & 63;
+  const uint16_t* q = a.q + static_cast<int64_t>(token) * a.q_stride + static_cast<int64_t>(head) * D;
+  // a key's (or value's) place: element offset of its row, and index of its scale
+  auto place = [&](int t, int64_t stride, int64_t* line) {
+    if constexpr (KV == PromptKv::kDense) {
+      return static_cast<int64_t>(key0 + t) * stride + static_cast<int64_t>(hk) * D;
+    } else {
+      const uint32_t pg = static_cast<uint32_t>(a.table[static_cast<int64_t>(seq) * a.table_cols + (t >> a.page_shift)]);
+      const int64_t page = pg < static_cast<uint32_t>(a.num_pages) ? pg : 0;
+      *line = ((page * a.Hk + hk) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
+      return *line * D;
+    }
+  };
+  auto value = [](const void* p, int64_t i) {
+    if constexpr (KV == PromptKv::kPagedFp8) {
+      const uint32_t u = static_cast<const uint8_t*>(p)[i];
+      return bf_lo(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, false)) & 0xFFFFu);
+    } else {
+      return bf_lo(static_cast<const uint16_t*>(p)[i]);
+    }
+  };
+  const float scale2 = power_scale(a.scale), sign = a.scale < 0.0f ? -1.0f : 1.0f;
+  float m = kNegInf, l = 0.0f, acc[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) acc[j] = 0.0f;
+  for (int t = t0; t < t1; t += 64) {
+    float s = kNegInf;
+    int64_t line = 0;
+    if (t + lane < t1) {
+      const int64_t at = place(t + lane, a.k_stride, &line);
+      float dot = 0.0f;
+      for (int d = 0; d < D; ++d) dot = fmaf(bf_lo(q[d]), value(a.k, at + d), dot);
+      if constexpr (KV == PromptKv::kPagedFp8) dot *= a.k_scale[line];
+      s = sign * dot * scale2;
+    }
+    float top = s;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float next = fmaxf(m, top), base = next == kNegInf ? 0.0f : next;
+    const float keep = __builtin_amdgcn_exp2f(m - base), p = __builtin_amdgcn_exp2f(s - base);
+    float sum = p;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, 64);
+    m = next;
+    l = l * keep + sum;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) acc[j] *= keep;
+    for (int i = 0; i < min(64, t1 - t); ++i) {
+      const int64_t at = place(t + i, a.v_stride, &line);
+      float w = __shfl(p, i, 64);
+      if constexpr (KV == PromptKv::kPagedFp8) w *= a.v_scale[line];
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) acc[j] = fmaf(w, value(a.v, at + lane * kPer + j), acc[j]);
+    }
+  }
+  if (bad) l = __builtin_nanf("");
+  const int64_t row = static_cast<int64_t>(token) * a.Hq + head;
+  if (parts > 1) {
+    const int64_t all = a.T * a.Hq, r = part * all + row;
+    if (lane == 0) *reinterpret_cast<float2*>(a.ws + parts * all * D + 2 * r) = float2{m, l};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) a.ws[r * D + lane * kPer + j] = acc[j];
+  } else {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (a.lse != nullptr && lane == 0) a.lse[row] = log_sum(m, l);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) a.out[row * D + lane * kPer + j] = static_cast<uint16_t>(pack_bf16(acc[j] * inv, 0.0f));
+  }
+}
+
+template <int D, int QG, PromptKv KV>
+__global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt_attention_kernel(
+    const PromptArgs a, int tiles, int chunk, int parts) {
+  using Z = Sizes<D, QG, KV>;
+  constexpr bool kFp8 = KV == PromptKv::kPagedFp8, kPaged = KV != PromptKv::kDense;
+  constexpr int kKeys = Z::kKeys, kSub = kKeys / 32, kSteps = D / 16, kOut = D / 32, kWaveRows = kKeys / 4;
+  constexpr int kBytes = kFp8 ? 1 : 2;                 // of a cached value
+  constexpr int kPerRow = D * kBytes / 16;             // 16-byte pieces of a cached row
+  constexpr int kLoads = kWaveRows * kPerRow / 64;     // transfers of a wave for a step's keys (and its values)
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * Z::kStage];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 31, lh = lane >> 5;
+  const int G = a.Hq / a.Hk;
+  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  const int part = rest / tiles;
+  const Place at = find_tile(a, G, Z::kCols, rest % tiles);
+  if (at.seq < 0) return;
+
+  // the sequence's keys
+  int key0 = 0, nk;
+  if constexpr (kPaged) {
+    nk = min(max(a.lens[at.seq], 0), a.max_len);
+  } else {
+    rows_of(a.k_starts, a.Tk, at.seq, &key0, &nk);
+    key0 = __builtin_amdgcn_readfirstlane(key0);
+  }
+  nk = __builtin_amdgcn_readfirstlane(nk);
+  const int cols = at.rows * G, col0 = at.tile * Z::kCols, wcol = col0 + wave * 32 * QG;
+  const bool busy = wcol < cols;
+  auto limit = [&](int col) { return a.causal ? min(max(nk - at.rows + col / G + 1, 0), nk) : nk; };
+  const int block_end = limit(min(col0 + Z::kCols, cols) - 1);
+  const int wave_end = limit(min(wcol + 32 * QG, cols) - 1), wave_all = limit(min(wcol, cols - 1));
+  const int t_begin = min(static_cast<int64_t>(part) * chunk, static_cast<int64_t>(block_end));
+  const int t_end = min(block_end - t_begin, chunk) + t_begin;
+  const int steps = (t_end - t_begin + kKeys - 1) / kKeys;
+
+  // queries
+  int64_t row[QG];
+  int lim[QG];
+  bf16x8 q[QG][kSteps];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const int col = min(wcol + 32 * g + li, cols - 1), token = col / G, head = hk * G + col - token * G;
+    lim[g] = limit(col);
+    row[g] = static_cast<int64_t>(at.row0 + token) * a.Hq + head;
+    const uint16_t* src = a.q + static_cast<int64_t>(at.row0 + token) * a.q_stride + static_cast<int64_t>(head) * D + 8 * lh;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) {
+      u32x4 v = *reinterpret_cast<const u32x4*>(src + 16 * c);
+      if (a.scale < 0.0f) v ^= 0x80008000u;  // so that scores grow with their products
+      q[g][c] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  f32x16 o[kOut][QG];
+  float m[QG], l[QG];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    m[g] = kNegInf, l[g] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][g][i] = 0.0f;
+  }
+  const float scale2 = power_scale(a.scale);
+
+  // Transfers: wave w brings rows [w kWaveRows, (w + 1) kWaveRows) of a step.
+  const uint32_t lds0 = lds_addr(lds);
+  const int64_t k_row_bytes = kPaged ? D * kBytes : a.k_stride * 2, v_row_bytes = kPaged ? D * kBytes : a.v_stride * 2;
+  uint32_t k_off[kLoads], v_off[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int r = i * (64 / kPerRow) + lane / kPerRow, c = lane % kPerRow, rr = wave * kWaveRows + r;
+    if constexpr (kFp8) {
+      k_off[i] = v_off[i] = r * D + 16 * c;
+    } else {
+      k_off[i] = static_cast<uint32_t>(r * k_row_bytes) + 16 * key_slot<D>(rr, c);
+      v_off[i] = static_cast<uint32_t>(r * v_row_bytes) + 16 * value_slot<D>(rr, c);
+    }
+  }
+  const uniform_i32 table = (uniform_i32)(a.table + static_cast<int64_t>(at.seq) * a.table_cols);
+  bool bad = false;
+  auto page_of = [&](int t) __attribute__((always_inline)) { return t < t_end ? table[t >> a.page_shift] : 0; };
+  int page_next = 0;
+  if constexpr (kPaged) page_next = page_of(t_begin + wave * kWaveRows);
+  struct Src {
+    const uint8_t *k, *v;
+    int64_t line;  // paged: index of the first row
+    int rows;
+  };
+  auto source = [&](int t0) __attribute__((always_inline)) {
+    Src s;
+    const int t = t0 + wave * kWaveRows;
+    s.rows = min(max(t_end - t, 0), kWaveRows);
+    s.line = 0;
+    if constexpr (kPaged) {
+      int pg = page_next;
+      page_next = page_of(t + kKeys);
+      if (s.rows > 0 && static_cast<uint32_t>(pg) >= static_cast<uint32_t>(a.num_pages)) bad = true, s.rows = 0;
+      if (s.rows == 0) pg = 0;
+      s.line = ((static_cast<int64_t>(pg) * a.Hk + hk) << a.page_shift) + (s.rows ? t & ((1 << a.page_shift) - 1) : 0);
+      s.k = static_cast<const uint8_t*>(a.k) + s.line * (D * kBytes);
+      s.v = static_cast<const uint8_t*>(a.v) + s.line * (D * kBytes);
+    } else {
+      const int64_t r = key0 + (s.rows ? t : 0);
+      s.k = static_cast<const uint8_t*>(a.k) + r * k_row_bytes + static_cast<int64_t>(hk) * D * 2;
+      s.v = static_cast<const uint8_t*>(a.v) + r * v_row_bytes + static_cast<int64_t>(hk) * D * 2;
+    }
+    return s;
+  };
+  auto span = [&](const Src& s, int64_t row_bytes) __attribute__((always_inline)) {
+    return s.rows == 0 ? 0 : static_cast<int>((s.rows - 1) * row_bytes + D * kBytes);
+  };
+  // bf16: straight into LDS
+  auto issue = [&](int buf, int t0) __attribute__((always_inline)) {
+    const Src s = source(t0);
+    const Rsrc rk = make_rsrc(s.k, span(s, k_row_bytes)), rv = make_rsrc(s.v, span(s, v_row_bytes));
+    const uint32_t dst = lds0 + buf * Z::kStage + wave * kWaveRows * Z::kRow;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) dma16(rk, dst + 1024 * i, k_off[i], 0);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) dma16(rv, dst + Z::kHalf + 1024 * i, v_off[i], 0);
+  };
+  // e4m3: through registers, widened to bf16 (exactly) on the way
+  u32x4 kr[kFp8 ? kLoads : 1], vr[kFp8 ? kLoads : 1];
+  float sr = 0.0f;
+  auto fetch = [&](int t0) __attribute__((always_inline)) {
+    if constexpr (kFp8) {
+      const Src s = source(t0);
+      const int n = span(s, D);
+      const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.k), 0, n, kRawBuffer);
+      const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.v), 0, n, kRawBuffer);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off[i], 0, 0));
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, v_off[i], 0, 0));
+      // lanes 0 .. 31 a scale of a key each, 32 .. 63 of a value
+      sr = li < s.rows ? (lh ? a.v_scale : a.k_scale)[s.line + li] : 0.0f;
+    }
+  };
+  auto put = [&](int buf) __attribute__((always_inline)) {
+    if constexpr (kFp8) {
+      uint8_t* base = lds + buf * Z::kStage;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int rr = wave * kWaveRows + i * (64 / kPerRow) + lane / kPerRow, c = 2 * (lane % kPerRow);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 kk, vv;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            kk[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kr[i][2 * h + j], 1.0f, false));
+            kk[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kr[i][2 * h + j], 1.0f, true));
+            vv[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(vr[i][2 * h + j], 1.0f, false));
+            vv[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(vr[i][2 * h + j], 1.0f, true));
+          }
+          *reinterpret_cast<u32x4*>(base + rr * Z::kRow + 16 * key_slot<D>(rr, c + h)) = kk;
+          *reinterpret_cast<u32x4*>(base + Z::kHalf + rr * Z::kRow + 16 * value_slot<D>(rr, c + h)) = vv;
+        }
+      }
+      if (li < kWaveRows)
+        *reinterpret_cast<float*>(base + 2 * Z::kHalf + 4 * (lh * kKeys + wave * kWaveRows + li)) = sr;
+    }
+  };
+
+  // Where a lane reads: key rows li (+ 32), 16-byte chunk 2 step + lh; of the
+  // values, for the transposing read, four rows 4 lh + li / 4 % 4 of 16 and of
+  // these the 8 bytes li % 4 of the 16 columns li / 16.
+  uint32_t k_at[kSteps], v_at[kOut];
+#pragma unroll
+  for (int c = 0; c < kSteps; ++c) k_at[c] = li * Z::kRow + 16 * key_slot<D>(li, 2 * c + lh);
+#pragma unroll
+  for (int t = 0; t < kOut; ++t) {
+    const int r = 4 * lh + (lane & 15) / 4;
+    v_at[t] = Z::kHalf + r * Z::kRow + 16 * value_slot<D>(r, 4 * t + 2 * (li / 16) + (lane & 3) / 2) + 8 * (lane & 1);
+  }
+  auto value_frag = [&](const uint8_t* base, int t, int k16) __attribute__((always_inline)) {
+    const uint8_t* p = base + v_at[t] + k16 * 16 * Z::kRow;
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(p));
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(p + 8 * Z::kRow));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  bool leaked = false;
+  auto step = [&](const uint8_t* base, int t0) __attribute__((always_inline)) {
+    f32x16 s[kSub][QG];
+#pragma unroll
+    for (int n = 0; n < kSub; ++n) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][g][i] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c) {
+        const bf16x8 k = *reinterpret_cast<const bf16x8*>(base + k_at[c] + n * 32 * Z::kRow);
+#pragma unroll
+        for (int g = 0; g < QG; ++g) s[n][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[g][c], s[n][g], 0, 0, 0);
+      }
+    }
+    const bool masked = t0 + kKeys > wave_all;
+    if constexpr (kFp8) {
+#pragma unroll
+      for (int n = 0; n < kSub; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 f = *reinterpret_cast<const f32x4*>(base + 2 * Z::kHalf + 4 * (32 * n + 2 * i + 4 * lh));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int g = 0; g < QG; ++g) s[n][g][i + j] *= f[j];
+        }
+    }
+    if (masked) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        const int rel = lim[g] - t0 - 4 * lh;
+#pragma unroll
+        for (int n = 0; n < kSub; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (32 * n + 8 * (i / 4) + i % 4 >= rel) s[n][g][i] = kNegInf;
+      }
+    }
+    bf16x8 p[kKeys / 16][QG];
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      float top = s[0][g][0];
+#pragma unroll
+      for (int n = 0; n < kSub; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][g][i]);
+      top = max_halves(top) * scale2;
+      const bool more = top > m[g] + 8.0f;
+      if (__any(more)) {
+        const float keep = more ? __builtin_amdgcn_exp2f(m[g] - top) : 1.0f;
+        m[g] = more ? top : m[g];
+        l[g] *= keep;
+#pragma unroll
+        for (int t = 0; t < kOut; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[t][g][i] *= keep;
+      }
+      const float base_m = m[g] == kNegInf ? 0.0f : m[g];
+#pragma unroll
+      for (int n = 0; n < kSub; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[n][g][i], scale2, -base_m));
+          l[g] += e;
+          s[n][g][i] = e;
+        }
+    }
+    if constexpr (kFp8) {
+#pragma unroll
+      for (int n = 0; n < kSub; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 f = *reinterpret_cast<const f32x4*>(base + 2 * Z::kHalf + 4 * (kKeys + 32 * n + 2 * i + 4 * lh));
+#pragma unroll
+          for (int g = 0; g < QG; ++g) {
+            const int rel = masked ? lim[g] - t0 - 4 * lh : kKeys;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              s[n][g][i + j] = 32 * n + 2 * i + j < rel ? s[n][g][i + j] * f[j] : 0.0f;
+          }
+        }
+    }
+#pragma unroll
+    for (int k16 = 0; k16 < kKeys / 16; ++k16)
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        float e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = s[k16 / 2][g][8 * (k16 & 1) + j];
+        p[k16][g] = __builtin_bit_cast(bf16x8, pack8_bf16(e));
+      }
+    if (masked && a.causal) {
+      // An infinity or NaN among these values reaches, through a weight of 0,
+      // also columns that do not see its token.
+      uint32_t hit = 0;
+      for (int i = lane; i < Z::kHalf / 16; i += 64) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(base + Z::kHalf + 16 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) hit |= (v[j] & 0x7FFF7FFFu) + 0x00800080u;
+      }
+      leaked |= __any((hit & 0x80008000u) != 0) != 0;
+    }
+#pragma unroll
+    for (int k16 = 0; k16 < kKeys / 16; ++k16)
+#pragma unroll
+      for (int t = 0; t < kOut; ++t) {
+        const bf16x8 v = value_frag(base, t, k16);
+#pragma unroll
+        for (int g = 0; g < QG; ++g) o[t][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k16][g], o[t][g], 0, 0, 0);
+      }
+  };
+
+  if (steps > 0) {
+    if constexpr (kFp8) {
+      fetch(t_begin);
+      put(0);
+      if (steps > 1) fetch(t_begin + kKeys);
+    } else {
+      issue(0, t_begin);
+    }
+  }
+  for (int i = 0; i < steps; ++i) {
+    const int t0 = t_begin + i * kKeys;
+    if constexpr (!kFp8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (i + 1 < steps) {
+      if constexpr (kFp8) {
+        put((i + 1) & 1);
+        if (i + 2 < steps) fetch(t0 + 2 * kKeys);
+      } else {
+        issue((i + 1) & 1, t0 + kKeys);
+      }
+    }
+    if (busy && t0 < wave_end) step(lds + (i & 1) * Z::kStage, t0);
+  }
+  if constexpr (kPaged) bad = __syncthreads_or(bad);
+  if (!busy) return;
+  if (leaked) {
+    for (int i = 0; i < 32 * QG && wcol + i < cols; ++i) {
+      const int col = wcol + i, token = col / G;
+      one_column<D, KV>(a, at.seq, at.row0 + token, hk * G + col - token * G, hk, key0, t_begin, min(t_end, limit(col)),
+                        part, parts, bad);
+    }
+    return;
+  }
+
+  // results: lane (li, lh) has values 32 t + 8 (i / 4) + 4 lh + i % 4 of its columns
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    l[g] = sum_halves(l[g]);
+    if (bad) l[g] = __builtin_nanf("");
+    if (wcol + 32 * g + li >= cols) continue;
+    if (parts > 1) {
+      const int64_t all = a.T * a.Hq, r = part * all + row[g];
+      if (lh == 0) *reinterpret_cast<float2*>(a.ws + parts * all * D + 2 * r) = float2{m[g], l[g]};
+      if (steps <= 0) continue;
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(a.ws + r * D + 32 * t + 2 * i + 4 * lh) =
+              f32x4{o[t][g][i], o[t][g][i + 1], o[t][g][i + 2], o[t][g][i + 3]};
+    } else {
+      const float inv = l[g] == 0.0f ? 0.0f : 1.0f / l[g];
+      if (a.lse != nullptr && lh == 0) a.lse[row[g]] = log_sum(m[g], l[g]);
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<u32x2*>(a.out + row[g] * D + 32 * t + 2 * i + 4 * lh) =
+              u32x2{pack_bf16(o[t][g][i] * inv, o[t][g][i + 1] * inv), pack_bf16(o[t][g][i + 2] * inv, o[t][g][i + 3] * inv)};
+    }
+  }
+}
+
+// Joins the parts of the key axis: D / 4 lanes a row of the packed queries.  A
+// part that a row's block did not reach has a maximum of -inf and a sum of 0.
+template <int D>
+__global__ __launch_bounds__(kThreads) void prompt_join_kernel(const PromptArgs a, int parts) {
+  constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
+  const int64_t all = a.T * a.Hq;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kLanes;
+  const int d = 4 * (threadIdx.x % kLanes);
+  // rows that no sequence has stay as they are
+  const int64_t first = static_cast<int64_t>(max(a.starts[0], 0)) * a.Hq, last = static_cast<int64_t>(a.starts[a.B]) * a.Hq;
+  if (row >= all || row < first || row >= last) return;
+  float top = kNegInf, sum = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  for (int i = 0; i < parts; ++i) {
+    const int64_t r = i * all + row;
+    const float2 ml = *reinterpret_cast<const float2*>(a.ws + parts * all * D + 2 * r);
+    if (ml.y == 0.0f) continue;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a.ws + r * D + d);
+    const float next = fmaxf(top, ml.x), base = next == kNegInf ? 0.0f : next;
+    const float keep = __builtin_amdgcn_exp2f(top - base), f = __builtin_amdgcn_exp2f(ml.x - base);
+    sum = sum * keep + f * ml.y;
+    acc = acc * keep + f * v;
+    top = next;
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  *reinterpret_cast<u32x2*>(a.out + row * D + d) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+  if (a.lse != nullptr && d == 0) a.lse[row] = log_sum(top, sum);
+}
+
+template <int D, int QG, PromptKv KV>
+void launch_tiles(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(p.tiles * a.Hk * p.parts));
+  hipLaunchKernelGGL((prompt_attention_kernel<D, QG, KV>), grid, dim3(kThreads), 0, st, a, static_cast<int>(p.tiles),
+                     static_cast<int>(p.chunk), p.parts);
+}
+
+template <int D, PromptKv KV>
+hipError_t launch_d(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
+  if constexpr (D < 256) {
+    if (p.cols == 256) launch_tiles<D, 2, KV>(a, p, st);
+    else launch_tiles<D, 1, KV>(a, p, st);
+  } else {
+    launch_tiles<D, 1, KV>(a, p, st);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  const int64_t per = kThreads / (D / 4);
+  hipLaunchKernelGGL((prompt_join_kernel<D>), dim3(static_cast<unsigned>((a.T * a.Hq + per - 1) / per)), dim3(kThreads), 0,
+                     st, a, p.parts);
+  return hipGetLastError();
+}
+
+template <PromptKv KV>
+hipError_t launch_kv(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
+  switch (a.D) {
+    case 64: return launch_d<64, KV>(a, p, st);
+    case 128: return launch_d<128, KV>(a, p, st);
+    default: return launch_d<256, KV>(a, p, st);
+  }
+}
+
+}  // namespace
+
+PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
+  const int64_t G = Hq / Hk;
+  PromptPlan p;
+  auto tiles = [&](int64_t cols) { return T * G / cols + std::min(B, T); };  // the most that B sequences of T tokens have
+  constexpr int64_t kCus = 256;
+  p.cols = D < 256 && tiles(256) * Hk >= kCus ? 256 : 128;
+  p.tiles = tiles(p.cols);
+  const int64_t blocks = p.tiles * Hk;
+  constexpr int64_t kLeast = 256;  // keys of a part
+  int64_t parts = std::max<int64_t>(1, std::min((2 * kCus + blocks / 2) / blocks, (max_len + kLeast - 1) / kLeast));
+  const int64_t each = (max_len + parts - 1) / parts;
+  p.chunk = (each + 63) / 64 * 64;
+  p.parts = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
+  return p;
+}
+
+hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t st) {
+  const PromptPlan p = prompt_plan(a.T, a.B, a.Hq, a.Hk, a.D, a.max_len);
+  switch (a.kv) {
+    case PromptKv::kDense: return launch_kv<PromptKv::kDense>(a, p, st);
+    case PromptKv::kPagedBf16: return launch_kv<PromptKv::kPagedBf16>(a, p, st);
+    default: return launch_kv<PromptKv::kPagedFp8>(a, p, st);
+  }
+}
+
+}  // namespace jq

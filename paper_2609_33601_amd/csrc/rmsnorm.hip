@@ -83,17 +83,6 @@ __device__ __forceinline__ void store_fp8(const NormArgs& a, int64_t row, int k,
   if (k % 128 == 0) a.scale[row * ((a.D + 127) / 128) + k / 128] = s;
 }
 
-__device__ __forceinline__ uint32_t int4_codes(const float* y, float s) {
-  uint32_t out = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float t = s == 0.0f ? 0.0f : __builtin_rintf(y[j] / s);
-    t = fminf(fmaxf(t, -8.0f), 7.0f);
-    out |= (static_cast<uint32_t>(static_cast<int>(t)) & 0xFu) << (4 * j);
-  }
-  return out;
-}
-
 // Rows of up to 8 * LPR elements: LPR lanes a row, 256 / LPR rows a block.
 template <int LPR, NormOut OUT, bool RES, bool NT>
 __global__ __launch_bounds__(256) void rmsnorm_short_kernel(const NormArgs a) {

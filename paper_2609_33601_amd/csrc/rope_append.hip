@@ -1,6 +1,8 @@
 // Rotation of the new tokens' queries and keys by their positions, and their
-// keys and values written into a paged cache, for gfx950.
+// keys and values written into a paged cache, for gfx950; with or without an
+// RMS norm of each head of the queries and keys before it (NORM).
 //
+//   x = (x r) w,  r = 1 / sqrt(mean over the head of x^2 + eps)   (NORM)
 //   (a, b) -> (a c - b s, a s + b c),  c = cos[position, i], s = sin[position, i]
 //   on the pairs (i, i + R/2), or (2i, 2i + 1) if interleaved, i < R/2; the
 //   other D - R elements of a head pass unchanged.  Values are not rotated.
@@ -26,10 +28,20 @@ namespace {
 
 using namespace block_detail;
 
+// Sum over the LPH lanes of a head, left in each.
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+  if constexpr (LPH >= 8) return lanes_sum<LPH>(v);
+  if constexpr (LPH >= 2) v += __uint_as_float(dpp<kDppXor1>(__float_as_uint(v)));
+  if constexpr (LPH >= 4) v += __uint_as_float(dpp<kDppXor2>(__float_as_uint(v)));
+  return v;
+}
+
 // LPH lanes a head: D / 16 rounded up to a power of two.
-template <int LPH, bool FP8, bool INTERLEAVED>
+template <int LPH, bool FP8, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
-  const int per_token = a.Hq + 2 * a.Hk;
+  // without a cache the values are not touched
+  const int per_token = a.Hq + (NORM && a.k_cache == nullptr ? 1 : 2) * a.Hk;
   const int64_t heads = a.T * per_token;
   const int c = threadIdx.x % LPH;  // 16 elements: 8 pairs, or 16 in a row
   constexpr int kHeads = 256 / LPH;
@@ -49,7 +61,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
     const int i0 = turned && !INTERLEAVED ? 8 * c : 16 * c;
     const int i1 = turned && !INTERLEAVED ? half + 8 * c : 16 * c + 8;
     const int64_t pos = live ? a.positions[t] : 0;
-    const int64_t slot = live && !is_q ? a.slots[t] : 0;
+    const int64_t slot = !live || is_q ? 0 : NORM && a.k_cache == nullptr ? -1 : a.slots[t];
     const bool pos_ok = pos >= 0 && pos < a.P;
     float f[16];
 #pragma unroll
@@ -57,6 +69,23 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
     if (live) {
       unpack8_bf16(*reinterpret_cast<const u32x4*>(src + i0), f);
       unpack8_bf16(*reinterpret_cast<const u32x4*>(src + i1), f + 8);
+    }
+    if constexpr (NORM) {
+      float ss = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) ss = fmaf(f[j], f[j], ss);
+      ss = head_sum<LPH>(ss);  // all lanes of the wave take part
+      const float r = 1.0f / sqrtf(ss / static_cast<float>(a.D) + a.eps);
+      if (live && !is_v) {
+        const uint16_t* weight = is_q ? a.q_weight : a.k_weight;
+        float w[16];
+        unpack8_bf16(*reinterpret_cast<const u32x4*>(weight + i0), w);
+        unpack8_bf16(*reinterpret_cast<const u32x4*>(weight + i1), w + 8);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f[j] = (f[j] * r) * w[j];
+      }
+    }
+    if (live) {
       if (turned) {
         // a position outside the tables has no rotation: NaN
         const int64_t row = (pos_ok ? pos : 0) * half + 8 * c;
@@ -79,6 +108,13 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
     if (is_q) {
       if (live) {
         uint16_t* dst = a.q_out + t * a.q_out_stride + static_cast<int64_t>(hk) * a.D;
+        *reinterpret_cast<u32x4*>(dst + i0) = pack8_bf16(f);
+        *reinterpret_cast<u32x4*>(dst + i1) = pack8_bf16(f + 8);
+      }
+    }
+    if constexpr (NORM) {
+      if (live && a.k_out != nullptr && !is_q && !is_v) {
+        uint16_t* dst = a.k_out + t * a.k_out_stride + static_cast<int64_t>(hk) * a.D;
         *reinterpret_cast<u32x4*>(dst + i0) = pack8_bf16(f);
         *reinterpret_cast<u32x4*>(dst + i1) = pack8_bf16(f + 8);
       }
@@ -109,32 +145,36 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
   }
 }
 
-template <int LPH>
+template <int LPH, bool NORM>
 hipError_t launch(const AppendArgs& a, hipStream_t st) {
-  const int64_t heads = a.T * (a.Hq + 2 * a.Hk);
+  const int64_t heads = a.T * (a.Hq + (a.k_cache == nullptr ? 1 : 2) * a.Hk);
   const int64_t blocks = (heads + 256 / LPH - 1) / (256 / LPH);
   constexpr int64_t kMostBlocks = 1 << 20;
   const dim3 grid(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks)), block(256);
   if (a.fp8) {
-    if (a.interleaved) hipLaunchKernelGGL((rope_append_kernel<LPH, true, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rope_append_kernel<LPH, true, false>), grid, block, 0, st, a);
+    if (a.interleaved) hipLaunchKernelGGL((rope_append_kernel<LPH, true, true, NORM>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rope_append_kernel<LPH, true, false, NORM>), grid, block, 0, st, a);
   } else {
-    if (a.interleaved) hipLaunchKernelGGL((rope_append_kernel<LPH, false, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rope_append_kernel<LPH, false, false>), grid, block, 0, st, a);
+    if (a.interleaved) hipLaunchKernelGGL((rope_append_kernel<LPH, false, true, NORM>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rope_append_kernel<LPH, false, false, NORM>), grid, block, 0, st, a);
   }
   return hipGetLastError();
 }
 
-}  // namespace
-
-hipError_t launch_rope_append(const AppendArgs& a, hipStream_t st) {
+template <bool NORM>
+hipError_t launch(const AppendArgs& a, hipStream_t st) {
   switch ((a.D + 15) / 16) {
-    case 1: return launch<1>(a, st);
-    case 2: return launch<2>(a, st);
-    case 3: case 4: return launch<4>(a, st);
-    case 5: case 6: case 7: case 8: return launch<8>(a, st);
-    default: return launch<16>(a, st);
+    case 1: return launch<1, NORM>(a, st);
+    case 2: return launch<2, NORM>(a, st);
+    case 3: case 4: return launch<4, NORM>(a, st);
+    case 5: case 6: case 7: case 8: return launch<8, NORM>(a, st);
+    default: return launch<16, NORM>(a, st);
   }
 }
+
+}  // namespace
+
+hipError_t launch_rope_append(const AppendArgs& a, hipStream_t st) { return launch<false>(a, st); }
+hipError_t launch_norm_rope_append(const AppendArgs& a, hipStream_t st) { return launch<true>(a, st); }
 
 }  // namespace jq

@@ -1,8 +1,9 @@
 """Python binding of the decoder block's other operators (include/jq_block.h).
 
 What a served block runs around its W4A4 linears (jq.py): the RMS norm that
-feeds a quantised linear, the 8-bit linear, the rotation of new queries and
-keys with their append to a paged cache, and attention over that cache.  As in
+feeds a quantised linear, the 8-bit linear, the gated activation, the rotation
+of new queries and keys (with or without a norm of each head) with their append
+to a paged cache, and attention over that cache or over packed prompts.  As in
 jq.py, a call only turns GPU torch tensors into pointers and the current HIP
 stream (of the device that its tensors are on) and raises on a non-OK status;
 there is no other path.  The checks themselves are compiled (_jq_block.so,
@@ -36,9 +37,20 @@ SIGNATURES = {
     "jq_paged_attention_workspace_bytes": (_sz, [_i64] * 6),
     "jq_paged_attention": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _i64,
                                   _i64, _f, _int, _int, _vp, _vp, _vp, _sz, _vp]),
+    "jq_qk_norm_rope_append": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _f, _vp, _vp,
+                                      _vp, _i64, _i64, _int, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64,
+                                      _int, _vp]),
+    "jq_gated_act": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _int, _int, _vp, _vp, _vp]),
+    "jq_prompt_attention_workspace_bytes": (_sz, [_i64] * 6),
+    "jq_prompt_attention": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _f,
+                                   _int, _vp, _vp, _vp, _sz, _vp]),
+    "jq_chunk_attention_workspace_bytes": (_sz, [_i64] * 6),
+    "jq_chunk_attention": (_int, [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64,
+                                  _i64, _i64, _i64, _f, _int, _int, _vp, _vp, _vp, _sz, _vp]),
 }
 
 NORM_OUT = {"bf16": 0, "fp8": 1, "int4": 2}
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 NATIVE_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_jq_block.so")
 
@@ -151,3 +163,69 @@ def jq_paged_attention(q, k_cache, v_cache, page_table, lens, k_scale=None, v_sc
     """
     return _done(_native.paged_attention(q, k_cache, v_cache, page_table, lens, k_scale, v_scale, max_len, sm_scale,
                                          causal, out, lse, workspace, _stream(stream)), "jq_paged_attention")
+
+
+def jq_qk_norm_rope_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots=None, k_cache=None, v_cache=None,
+                           k_scale=None, v_scale=None, eps=1e-6, interleaved=False, dense_k=False, q_out=None,
+                           k_out=None, stream=None):
+    """jq_rope_append with an RMS norm of each head of q and k (weights bf16 [D]) before the rotation; returns (q, k).
+
+    q is the rotated q (q_out=q: in place; None where q is None).  k are the rotated keys as bf16 [T,Hk,D] where there
+    is no cache, where dense_k asks for them or where k_out takes them (k_out=k: in place), else None.  Without a cache
+    (k_cache, v_cache and slots None) v is not touched and may be None.
+    """
+    if k_cache is None and v_cache is None:
+        v = None
+    return _done(_native.qk_norm_rope_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots, k_cache, v_cache,
+                                             k_scale, v_scale, eps, interleaved, dense_k, q_out, k_out,
+                                             _stream(stream)), "jq_qk_norm_rope_append")
+
+
+def jq_gated_act(gate, up=None, act="silu", out="bf16", y=None, scale=None, stream=None):
+    """act(gate) * up of bf16 [M,N] (rows may be apart, as the halves of one projection's are); up = None: act(gate).
+
+    act is "silu", "gelu" or "gelu_tanh".  Returns a tuple as jq_rmsnorm does: out = "bf16": (y bf16 [M,N],); "fp8":
+    (y float8_e4m3fn [M,N], scale fp32 [M, ceil(N/128)]), the operand of jq_fp8_gemm; "int4": (y uint8 [M,N/2], scale
+    fp32 [M]), the operand of jq_w4a4_gemm.
+    """
+    kind, what = NORM_OUT.get(out), ACTS.get(act)
+    if kind is None:
+        raise ValueError(f"out must be one of {sorted(NORM_OUT)}, got {out!r}")
+    if what is None:
+        raise ValueError(f"act must be one of {sorted(ACTS)}, got {act!r}")
+    return _done(_native.gated_act(gate, up, what, kind, y, scale, _stream(stream)), "jq_gated_act")
+
+
+def jq_prompt_attention_workspace_bytes(T, Tk, B, Hq, Hk, D):
+    return int(lib().jq_prompt_attention_workspace_bytes(int(T), int(Tk), int(B), int(Hq), int(Hk), int(D)))
+
+
+def jq_prompt_attention(q, k, v, starts, k_starts=None, causal=True, sm_scale=None, out=None, lse=None, workspace=None,
+                        stream=None):
+    """Attention of packed sequences q [T,Hq,D] over their own keys and values k, v [Tk,Hk,D] (bf16, tokens may be
+    apart); returns bf16 [T,Hq,D].
+
+    Sequence b has the rows starts[b] .. starts[b+1] of q and k_starts[b] .. k_starts[b+1] of k and v (starts, k_starts
+    int32 [B+1]; k_starts = None: the same rows).  Causal: the last query of a sequence sees its last key, each one
+    before it one key less.  sm_scale is D**-0.5 by default; lse fp32 [T,Hq], if given, gets the logarithms of the
+    softmax denominators.  Rows of no sequence stay as they are (in a new out, whatever the memory held).
+    """
+    return _done(_native.prompt_attention(q, k, v, starts, k_starts, causal, sm_scale, out, lse, workspace,
+                                          _stream(stream)), "jq_prompt_attention")
+
+
+def jq_chunk_attention_workspace_bytes(T, B, Hq, Hk, D, max_len):
+    return int(lib().jq_chunk_attention_workspace_bytes(int(T), int(B), int(Hq), int(Hk), int(D), int(max_len)))
+
+
+def jq_chunk_attention(q, k_cache, v_cache, page_table, starts, lens, k_scale=None, v_scale=None, max_len=None,
+                       sm_scale=None, causal=True, out=None, lse=None, workspace=None, stream=None):
+    """Attention of chunks of new tokens, packed in q [T,Hq,D] (bf16, tokens may be apart), over each sequence's cached
+    tokens, the new ones among them; returns bf16 [T,Hq,D].
+
+    Sequence b has the rows starts[b] .. starts[b+1] (int32 [B+1]) of q, lens[b] (int32 [B]) cached tokens and the pages
+    page_table[b] (int32 [B,columns]).  max_len bounds the lengths (the table's capacity by default) and decides how the
+    cache is split; the rest is as at jq_prompt_attention.
+    """
+    return _done(_native.chunk_attention(q, k_cache, v_cache, page_table, starts, lens, k_scale, v_scale, max_len,
+                                         sm_scale, causal, out, lse, workspace, _stream(stream)), "jq_chunk_attention")
