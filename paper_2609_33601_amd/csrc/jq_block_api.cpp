@@ -109,19 +109,19 @@ size_t attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, 
 }
 
 // Sizes of jq_prompt_attention and jq_chunk_attention.
-jq_status check_prompt(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
+jq_status check_prompt(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
   if (T <= 0 || B <= 0 || Hq <= 0 || Hk <= 0 || max_len <= 0) return JQ_ERR_INVALID_ARG;
   if (Hq % Hk != 0 || (D != 64 && D != 128 && D != 256)) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (T > kMaxAxis || max_len > kMaxAxis || B > (1 << 20) || Hq > 65536) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (T * Hq >= (int64_t(1) << 31)) return JQ_ERR_UNSUPPORTED_SHAPE;
-  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len);
-  // grids of fewer than 2^24 blocks of 256 threads
-  return p.tiles * Hk * p.parts < kMaxBlocks ? JQ_OK : JQ_ERR_UNSUPPORTED_SHAPE;
+  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len, paged);
+  // grids of fewer than 2^24 blocks of 256 threads (an 8-bit cache takes 128 columns where others take 256)
+  return (p.cols == 256 ? 2 : 1) * p.tiles * Hk * p.parts < kMaxBlocks ? JQ_OK : JQ_ERR_UNSUPPORTED_SHAPE;
 }
 
-size_t prompt_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
-  if (check_prompt(T, B, Hq, Hk, D, max_len) != JQ_OK) return 0;
-  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len);
+size_t prompt_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
+  if (check_prompt(T, B, Hq, Hk, D, max_len, paged) != JQ_OK) return 0;
+  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len, paged);
   if (p.parts == 1) return 0;
   const size_t rows = static_cast<size_t>(T) * static_cast<size_t>(Hq) * p.parts;
   return round_up(rows * (static_cast<size_t>(D) + 2) * sizeof(float), kWsAlign);
@@ -129,14 +129,14 @@ size_t prompt_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int6
 
 // What the two calls share: the queries, their starts, outputs and workspace.
 jq_status check_prompt_call(const void* q, int64_t q_stride, const int32_t* starts, int64_t T, int64_t B, int64_t Hq,
-                            int64_t Hk, int64_t D, int64_t max_len, const void* out, const float* lse,
+                            int64_t Hk, int64_t D, int64_t max_len, bool paged, const void* out, const float* lse,
                             const void* workspace, size_t workspace_bytes) {
   if (q == nullptr || starts == nullptr || out == nullptr) return JQ_ERR_INVALID_ARG;
-  jq_status st = check_prompt(T, B, Hq, Hk, D, max_len);
+  jq_status st = check_prompt(T, B, Hq, Hk, D, max_len, paged);
   if (st == JQ_OK) st = check_stride(q_stride, Hq * D);
   if (st != JQ_OK) return st;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(starts, 4) || !aligned(lse, 4)) return JQ_ERR_MISALIGNED;
-  const size_t need = prompt_workspace_bytes(T, B, Hq, Hk, D, max_len);
+  const size_t need = prompt_workspace_bytes(T, B, Hq, Hk, D, max_len, paged);
   if (need > 0) {
     if (workspace == nullptr) return JQ_ERR_INVALID_ARG;
     if (!aligned(workspace, kWsAlign)) return JQ_ERR_MISALIGNED;
@@ -369,7 +369,7 @@ jq_status jq_gated_act(const void* gate, int64_t gate_stride, const void* up, in
 }
 
 size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int64_t Hq, int64_t Hk, int64_t D) {
-  return prompt_workspace_bytes(T, B, Hq, Hk, D, Tk);
+  return prompt_workspace_bytes(T, B, Hq, Hk, D, Tk, false);
 }
 
 jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
@@ -377,7 +377,7 @@ jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, in
                               int64_t B, int64_t Hq, int64_t Hk, int64_t D, float sm_scale, int causal, void* out,
                               float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (k == nullptr || v == nullptr) return JQ_ERR_INVALID_ARG;
-  jq_status st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, Tk, out, lse, workspace, workspace_bytes);
+  jq_status st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, Tk, false, out, lse, workspace, workspace_bytes);
   if (st == JQ_OK) st = check_key_stride(k_stride, Hk * D);
   if (st == JQ_OK) st = check_key_stride(v_stride, Hk * D);
   if (st != JQ_OK) return st;
@@ -393,7 +393,7 @@ jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, in
 }
 
 size_t jq_chunk_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
-  return prompt_workspace_bytes(T, B, Hq, Hk, D, max_len);
+  return prompt_workspace_bytes(T, B, Hq, Hk, D, max_len, true);
 }
 
 jq_status jq_chunk_attention(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
@@ -404,7 +404,7 @@ jq_status jq_chunk_attention(const void* q, int64_t q_stride, const void* k_cach
                              size_t workspace_bytes, void* stream) {
   if (page_table == nullptr || lens == nullptr || table_cols <= 0) return JQ_ERR_INVALID_ARG;
   jq_status st = check_cache(Hk, k_cache, v_cache, k_scale, v_scale, num_pages, page_size, type);
-  if (st == JQ_OK) st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, max_len, out, lse, workspace, workspace_bytes);
+  if (st == JQ_OK) st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, max_len, true, out, lse, workspace, workspace_bytes);
   if (st != JQ_OK) return st;
   if (table_cols > kMaxAxis) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (max_len > table_cols * page_size) return JQ_ERR_INVALID_ARG;

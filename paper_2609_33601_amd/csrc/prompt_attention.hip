@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "block_common.h"
 #include "block_internal.h"
@@ -46,9 +47,11 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0.0f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
-// A block's place: a sequence, its rows in the packed tensors and its tile of columns.
+// A block's place: a sequence, its rows in the packed tensors, its tile of
+// columns, and its keys.
 struct Place {
   int seq, row0, rows, tile;
+  int key0, keys;  // rows of its own keys, or cached tokens
 };
 
 // The `index`-th tile of `per` columns, counted from the last one of the last
@@ -62,6 +65,7 @@ __device__ __forceinline__ void rows_of(const int32_t* starts, int64_t T, int b,
   *row0 = s0;
   *rows = max(s1 - s0, 0);
 }
+template <bool PAGED>
 __device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, int index) {
   const int lane = threadIdx.x & 63;
   auto tiles_of = [&](int b, int* row0, int* rows) {
@@ -69,11 +73,16 @@ __device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, 
     if (b < a.B) rows_of(a.starts, a.T, b, row0, rows);
     return (*rows * G + per - 1) / per;
   };
-  Place p{-1, 0, 0, 0};
+  Place p{-1, 0, 0, 0, 0, 0};
   int after = 0;  // tiles of the sequences behind
   for (int base = (a.B - 1) / 64 * 64; base >= 0; base -= 64) {
     int row0, rows;
     const int n = tiles_of(base + lane, &row0, &rows);
+    int key0 = 0, keys = 0;  // asked for with the rows, not after them
+    if (base + lane < a.B) {
+      if constexpr (PAGED) keys = min(max(a.lens[base + lane], 0), a.max_len);
+      else rows_of(a.k_starts, a.Tk, base + lane, &key0, &keys);
+    }
     int upto = n;  // tiles of this lane's sequence and those behind it, of these 64
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -88,6 +97,8 @@ __device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, 
       p.row0 = __builtin_amdgcn_readlane(row0, l);
       p.rows = __builtin_amdgcn_readlane(rows, l);
       p.tile = __builtin_amdgcn_readlane(n - 1 - mine, l);
+      p.key0 = __builtin_amdgcn_readlane(key0, l);
+      p.keys = __builtin_amdgcn_readlane(keys, l);
       return p;
     }
     after += __builtin_amdgcn_readlane(upto, 0);
@@ -110,12 +121,14 @@ __device__ __forceinline__ int value_slot(int row, int c) {
 
 template <int D, int QG, PromptKv KV>
 struct Sizes {
-  static constexpr int kKeys = D == 256 ? 32 : 64;  // keys of a step
+  static constexpr int kKeys = 64;                  // keys of a step
   static constexpr int kRow = 2 * D;                // bytes of a row in LDS
   static constexpr int kHalf = kKeys * kRow;        // a step's keys, or its values
   static constexpr int kStage = 2 * kHalf + (KV == PromptKv::kPagedFp8 ? 8 * kKeys : 0);
-  static constexpr int kCols = 4 * 32 * QG;         // columns of a block
-  static constexpr int kPerSimd = D == 64 || (D == 128 && QG == 1) ? 2 : 1;
+  static constexpr int kLane = QG * (D / 2 + 2);    // floats of a lane's result: outputs, maxima, sums
+  static constexpr int kJoin = 2 * 64 * 4 * kLane + 16;  // two waves' results, where halves of the keys are joined
+  static constexpr int kLds = 2 * kStage > kJoin ? 2 * kStage : kJoin;
+  static constexpr int kPerSimd = D <= 128 ? 2 : 1;
 };
 
 // One column's keys [t0, t1) by one wave, in fp32 and straight from memory: for
@@ -200,14 +213,14 @@ __device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int tok
 
 template <int D, int QG, PromptKv KV>
 __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt_attention_kernel(
-    const PromptArgs a, int tiles, int chunk, int parts) {
+    const PromptArgs a, int tiles, int per, int chunk, int parts) {
   using Z = Sizes<D, QG, KV>;
   constexpr bool kFp8 = KV == PromptKv::kPagedFp8, kPaged = KV != PromptKv::kDense;
-  constexpr int kKeys = Z::kKeys, kSub = kKeys / 32, kSteps = D / 16, kOut = D / 32, kWaveRows = kKeys / 4;
+  constexpr int kKeys = Z::kKeys, kSteps = D / 16, kOut = D / 32, kWaveRows = kKeys / 4;
   constexpr int kBytes = kFp8 ? 1 : 2;                 // of a cached value
   constexpr int kPerRow = D * kBytes / 16;             // 16-byte pieces of a cached row
   constexpr int kLoads = kWaveRows * kPerRow / 64;     // transfers of a wave for a step's keys (and its values)
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * Z::kStage];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Z::kLds];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -215,22 +228,18 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   const int G = a.Hq / a.Hk;
   const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
   const int part = rest / tiles;
-  const Place at = find_tile(a, G, Z::kCols, rest % tiles);
+  const Place at = find_tile<kPaged>(a, G, per, rest % tiles);
   if (at.seq < 0) return;
 
-  // the sequence's keys
-  int key0 = 0, nk;
-  if constexpr (kPaged) {
-    nk = min(max(a.lens[at.seq], 0), a.max_len);
-  } else {
-    rows_of(a.k_starts, a.Tk, at.seq, &key0, &nk);
-    key0 = __builtin_amdgcn_readfirstlane(key0);
-  }
-  nk = __builtin_amdgcn_readfirstlane(nk);
-  const int cols = at.rows * G, col0 = at.tile * Z::kCols, wcol = col0 + wave * 32 * QG;
+  const int key0 = at.key0, nk = at.keys;
+  const int cols = at.rows * G, col0 = at.tile * per, last_col = min(col0 + per, cols) - 1;
+  // A wave has 32 QG columns; where two waves have all of the tile's, the other
+  // two have the same ones, and each pair takes half of every step's keys.
+  const bool halves = last_col - col0 < 64 * QG;
+  const int wcol = col0 + (halves ? wave & 1 : wave) * 32 * QG;
   const bool busy = wcol < cols;
   auto limit = [&](int col) { return a.causal ? min(max(nk - at.rows + col / G + 1, 0), nk) : nk; };
-  const int block_end = limit(min(col0 + Z::kCols, cols) - 1);
+  const int block_end = limit(last_col);
   const int wave_end = limit(min(wcol + 32 * QG, cols) - 1), wave_all = limit(min(wcol, cols - 1));
   const int t_begin = min(static_cast<int64_t>(part) * chunk, static_cast<int64_t>(block_end));
   const int t_end = min(block_end - t_begin, chunk) + t_begin;
@@ -383,7 +392,13 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   };
 
   bool leaked = false;
-  auto step = [&](const uint8_t* base, int t0) __attribute__((always_inline)) {
+  // The keys t0 .. of a stage: all of them, or half `part` of them.
+  auto step = [&](const uint8_t* stage, int t0, int part, auto count, auto mask) __attribute__((always_inline)) {
+    constexpr int kSub = decltype(count)::value;
+    constexpr bool kMask = decltype(mask)::value;
+    const uint8_t* base = stage + part * 32 * Z::kRow;
+    const float* scales = reinterpret_cast<const float*>(stage + 2 * Z::kHalf) + 32 * part;
+    t0 += 32 * part;
     f32x16 s[kSub][QG];
 #pragma unroll
     for (int n = 0; n < kSub; ++n) {
@@ -398,20 +413,19 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         for (int g = 0; g < QG; ++g) s[n][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[g][c], s[n][g], 0, 0, 0);
       }
     }
-    const bool masked = t0 + kKeys > wave_all;
     if constexpr (kFp8) {
 #pragma unroll
       for (int n = 0; n < kSub; ++n)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          const f32x4 f = *reinterpret_cast<const f32x4*>(base + 2 * Z::kHalf + 4 * (32 * n + 2 * i + 4 * lh));
+          const f32x4 f = *reinterpret_cast<const f32x4*>(scales + 32 * n + 2 * i + 4 * lh);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int g = 0; g < QG; ++g) s[n][g][i + j] *= f[j];
         }
     }
-    if (masked) {
+    if constexpr (kMask) {
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
         const int rel = lim[g] - t0 - 4 * lh;
@@ -422,7 +436,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
             if (32 * n + 8 * (i / 4) + i % 4 >= rel) s[n][g][i] = kNegInf;
       }
     }
-    bf16x8 p[kKeys / 16][QG];
+    bf16x8 p[2 * kSub][QG];
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
       float top = s[0][g][0];
@@ -456,10 +470,10 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
       for (int n = 0; n < kSub; ++n)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          const f32x4 f = *reinterpret_cast<const f32x4*>(base + 2 * Z::kHalf + 4 * (kKeys + 32 * n + 2 * i + 4 * lh));
+          const f32x4 f = *reinterpret_cast<const f32x4*>(scales + kKeys + 32 * n + 2 * i + 4 * lh);
 #pragma unroll
           for (int g = 0; g < QG; ++g) {
-            const int rel = masked ? lim[g] - t0 - 4 * lh : kKeys;
+            const int rel = kMask ? lim[g] - t0 - 4 * lh : kKeys;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               s[n][g][i + j] = 32 * n + 2 * i + j < rel ? s[n][g][i + j] * f[j] : 0.0f;
@@ -467,7 +481,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         }
     }
 #pragma unroll
-    for (int k16 = 0; k16 < kKeys / 16; ++k16)
+    for (int k16 = 0; k16 < 2 * kSub; ++k16)
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
         float e[8];
@@ -475,11 +489,11 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         for (int j = 0; j < 8; ++j) e[j] = s[k16 / 2][g][8 * (k16 & 1) + j];
         p[k16][g] = __builtin_bit_cast(bf16x8, pack8_bf16(e));
       }
-    if (masked && a.causal) {
+    if (kMask && a.causal) {
       // An infinity or NaN among these values reaches, through a weight of 0,
       // also columns that do not see its token.
       uint32_t hit = 0;
-      for (int i = lane; i < Z::kHalf / 16; i += 64) {
+      for (int i = lane; i < 2 * kSub * Z::kRow; i += 64) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(base + Z::kHalf + 16 * i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) hit |= (v[j] & 0x7FFF7FFFu) + 0x00800080u;
@@ -487,7 +501,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
       leaked |= __any((hit & 0x80008000u) != 0) != 0;
     }
 #pragma unroll
-    for (int k16 = 0; k16 < kKeys / 16; ++k16)
+    for (int k16 = 0; k16 < 2 * kSub; ++k16)
 #pragma unroll
       for (int t = 0; t < kOut; ++t) {
         const bf16x8 v = value_frag(base, t, k16);
@@ -505,21 +519,77 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
       issue(0, t_begin);
     }
   }
-  for (int i = 0; i < steps; ++i) {
-    const int t0 = t_begin + i * kKeys;
+  auto arrive = [&](int i) __attribute__((always_inline)) {
     if constexpr (!kFp8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (i + 1 < steps) {
-      if constexpr (kFp8) {
-        put((i + 1) & 1);
-        if (i + 2 < steps) fetch(t0 + 2 * kKeys);
-      } else {
-        issue((i + 1) & 1, t0 + kKeys);
-      }
+    if (i + 1 >= steps) return;
+    if constexpr (kFp8) {
+      put((i + 1) & 1);
+      if (i + 2 < steps) fetch(t_begin + (i + 2) * kKeys);
+    } else {
+      issue((i + 1) & 1, t_begin + (i + 1) * kKeys);
     }
-    if (busy && t0 < wave_end) step(lds + (i & 1) * Z::kStage, t0);
-  }
+  };
+  auto run = [&](int part, auto count) __attribute__((always_inline)) {
+    // steps that every column sees whole; those that some see in part; the rest
+    const int first = t_begin + 32 * part;
+    const int plain = busy ? max(min(wave_all, t_end) - first + 64 - 32 * decltype(count)::value, 0) / kKeys : 0;
+    const int seen = busy ? max(min(wave_end, t_end) - first + kKeys - 1, 0) / kKeys : 0;
+    int i = 0;
+    for (; i < plain; ++i) {
+      arrive(i);
+      step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, part, count, std::false_type());
+    }
+    for (; i < seen; ++i) {
+      arrive(i);
+      step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, part, count, std::true_type());
+    }
+    for (; i < steps; ++i) arrive(i);
+  };
+  if (halves) run(wave >> 1, std::integral_constant<int, 1>());
+  else run(0, std::integral_constant<int, 2>());
   if constexpr (kPaged) bad = __syncthreads_or(bad);
+#pragma unroll
+  for (int g = 0; g < QG; ++g) l[g] = sum_halves(l[g]);
+  if (halves) {
+    // the second pair's results through LDS to the first
+    __syncthreads();
+    float* mine = reinterpret_cast<float*>(lds) + (wave & 1) * 64 * Z::kLane;
+    int* flag = reinterpret_cast<int*>(lds + Z::kJoin - 16) + (wave & 1);
+    if (wave >= 2) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+#pragma unroll
+        for (int t = 0; t < kOut; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4*>(mine + ((g * kOut + t) * 4 + i / 4) * 256 + 4 * lane) =
+                f32x4{o[t][g][i], o[t][g][i + 1], o[t][g][i + 2], o[t][g][i + 3]};
+        mine[QG * kOut * 1024 + 128 * g + lane] = m[g];
+        mine[QG * kOut * 1024 + 128 * g + 64 + lane] = l[g];
+      }
+      if (lane == 0) *flag = leaked;
+    }
+    __syncthreads();
+    if (wave >= 2) return;
+    leaked |= *flag != 0;
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      const float m1 = mine[QG * kOut * 1024 + 128 * g + lane], l1 = mine[QG * kOut * 1024 + 128 * g + 64 + lane];
+      const float top = fmaxf(m[g], m1), base = top == kNegInf ? 0.0f : top;
+      const float f0 = __builtin_amdgcn_exp2f(m[g] - base), f1 = __builtin_amdgcn_exp2f(m1 - base);
+      m[g] = top;
+      l[g] = l[g] * f0 + l1 * f1;
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(mine + ((g * kOut + t) * 4 + i / 4) * 256 + 4 * lane);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[t][g][i + j] = o[t][g][i + j] * f0 + v[j] * f1;
+        }
+    }
+  }
   if (!busy) return;
   if (leaked) {
     for (int i = 0; i < 32 * QG && wcol + i < cols; ++i) {
@@ -533,7 +603,6 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   // results: lane (li, lh) has values 32 t + 8 (i / 4) + 4 lh + i % 4 of its columns
 #pragma unroll
   for (int g = 0; g < QG; ++g) {
-    l[g] = sum_halves(l[g]);
     if (bad) l[g] = __builtin_nanf("");
     if (wcol + 32 * g + li >= cols) continue;
     if (parts > 1) {
@@ -559,45 +628,89 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   }
 }
 
-// Joins the parts of the key axis: D / 4 lanes a row of the packed queries.  A
-// part that a row's block did not reach has a maximum of -inf and a sum of 0.
-template <int D>
+// Joins the parts of the key axis: D / 4 lanes a row of the packed queries, and
+// SETS such groups that take the row's parts in turn.  A part that a row's
+// block did not reach has a sum of 0 and no outputs.
+template <int D, int SETS>
 __global__ __launch_bounds__(kThreads) void prompt_join_kernel(const PromptArgs a, int parts) {
-  constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
+  constexpr int kLanes = D / 4, kRows = kThreads / (kLanes * SETS), kBatch = 4;
+  __shared__ f32x4 red[SETS > 1 ? kThreads : 1];
+  __shared__ float2 red_ml[SETS > 1 ? kRows * SETS : 1];
   const int64_t all = a.T * a.Hq;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kLanes;
+  const int set = threadIdx.x / kLanes % SETS, r = threadIdx.x / (kLanes * SETS);
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + r;
   const int d = 4 * (threadIdx.x % kLanes);
+  const float2* ml = reinterpret_cast<const float2*>(a.ws + parts * all * D);
+  float top = kNegInf, sum = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  if (row < all) {
+    for (int i = set; i < parts; i += SETS * kBatch) {
+      // all loads of a batch on their way at once
+      float2 w[kBatch];
+      f32x4 v[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int64_t at = static_cast<int64_t>(min(i + j * SETS, parts - 1)) * all + row;
+        w[j] = ml[at];
+        v[j] = *reinterpret_cast<const f32x4*>(a.ws + at * D + d);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (i + j * SETS >= parts || w[j].y == 0.0f) continue;
+        const float next = fmaxf(top, w[j].x), base = next == kNegInf ? 0.0f : next;
+        const float keep = __builtin_amdgcn_exp2f(top - base), f = __builtin_amdgcn_exp2f(w[j].x - base);
+        sum = sum * keep + f * w[j].y;
+        acc = acc * keep + f * v[j];
+        top = next;
+      }
+    }
+  }
+  if constexpr (SETS > 1) {
+    red[threadIdx.x] = acc;
+    if (d == 0) red_ml[r * SETS + set] = float2{top, sum};
+    __syncthreads();
+    if (set) return;
+    for (int i = 1; i < SETS; ++i) top = fmaxf(top, red_ml[r * SETS + i].x);
+    const float base = top == kNegInf ? 0.0f : top;
+    sum = 0.0f;
+    acc = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < SETS; ++i) {
+      const float f = __builtin_amdgcn_exp2f(red_ml[r * SETS + i].x - base);
+      sum += f * red_ml[r * SETS + i].y;
+      acc += f * red[(r * SETS + i) * kLanes + d / 4];
+    }
+  }
   // rows that no sequence has stay as they are
   const int64_t first = static_cast<int64_t>(max(a.starts[0], 0)) * a.Hq, last = static_cast<int64_t>(a.starts[a.B]) * a.Hq;
   if (row >= all || row < first || row >= last) return;
-  float top = kNegInf, sum = 0.0f;
-  f32x4 acc = {0, 0, 0, 0};
-  for (int i = 0; i < parts; ++i) {
-    const int64_t r = i * all + row;
-    const float2 ml = *reinterpret_cast<const float2*>(a.ws + parts * all * D + 2 * r);
-    if (ml.y == 0.0f) continue;
-    const f32x4 v = *reinterpret_cast<const f32x4*>(a.ws + r * D + d);
-    const float next = fmaxf(top, ml.x), base = next == kNegInf ? 0.0f : next;
-    const float keep = __builtin_amdgcn_exp2f(top - base), f = __builtin_amdgcn_exp2f(ml.x - base);
-    sum = sum * keep + f * ml.y;
-    acc = acc * keep + f * v;
-    top = next;
-  }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   *reinterpret_cast<u32x2*>(a.out + row * D + d) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
   if (a.lse != nullptr && d == 0) a.lse[row] = log_sum(top, sum);
+}
+
+template <int D>
+void launch_join(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
+  const int64_t rows = a.T * a.Hq;
+  constexpr int kSets = 1024 / D;
+  const int64_t per = 1024 / D;  // rows of a block of one set
+  if (p.parts > 4 && rows < 8192) {
+    hipLaunchKernelGGL((prompt_join_kernel<D, kSets>), dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, st, a, p.parts);
+  } else {
+    hipLaunchKernelGGL((prompt_join_kernel<D, 1>), dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(kThreads), 0, st,
+                       a, p.parts);
+  }
 }
 
 template <int D, int QG, PromptKv KV>
 void launch_tiles(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>(p.tiles * a.Hk * p.parts));
   hipLaunchKernelGGL((prompt_attention_kernel<D, QG, KV>), grid, dim3(kThreads), 0, st, a, static_cast<int>(p.tiles),
-                     static_cast<int>(p.chunk), p.parts);
+                     p.cols, static_cast<int>(p.chunk), p.parts);
 }
 
 template <int D, PromptKv KV>
 hipError_t launch_d(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
-  if constexpr (D < 256) {
+  if constexpr (D == 64 && KV != PromptKv::kPagedFp8) {
     if (p.cols == 256) launch_tiles<D, 2, KV>(a, p, st);
     else launch_tiles<D, 1, KV>(a, p, st);
   } else {
@@ -605,9 +718,7 @@ hipError_t launch_d(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts == 1) return e;
-  const int64_t per = kThreads / (D / 4);
-  hipLaunchKernelGGL((prompt_join_kernel<D>), dim3(static_cast<unsigned>((a.T * a.Hq + per - 1) / per)), dim3(kThreads), 0,
-                     st, a, p.parts);
+  launch_join<D>(a, p, st);
   return hipGetLastError();
 }
 
@@ -622,16 +733,17 @@ hipError_t launch_kv(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
 
 }  // namespace
 
-PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
-  const int64_t G = Hq / Hk;
+PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
+  const int64_t G = Hq / Hk, expect = paged ? max_len : max_len / B;  // keys of a sequence
+  constexpr int64_t kSlots = 512, kLeast = 128;                       // blocks that run at once; keys of a part
+  auto blocks_of = [&](int64_t cols) { return std::max((T * G + cols - 1) / cols, B) * Hk; };
+  const bool lengthy = paged ? max_len >= 512 : expect >= 4096 || (expect >= 512 && max_len >= 4 * T);
   PromptPlan p;
-  auto tiles = [&](int64_t cols) { return T * G / cols + std::min(B, T); };  // the most that B sequences of T tokens have
-  constexpr int64_t kCus = 256;
-  p.cols = D < 256 && tiles(256) * Hk >= kCus ? 256 : 128;
-  p.tiles = tiles(p.cols);
-  const int64_t blocks = p.tiles * Hk;
-  constexpr int64_t kLeast = 256;  // keys of a part
-  int64_t parts = std::max<int64_t>(1, std::min((2 * kCus + blocks / 2) / blocks, (max_len + kLeast - 1) / kLeast));
+  p.cols = D == 64 && T * G / 256 * Hk >= kSlots ? 256 : lengthy || blocks_of(128) >= 384 ? 128 : 64;
+  p.tiles = T * G / p.cols + std::min(B, T);  // the most that B sequences of T tokens have
+  int64_t parts = 1;
+  if (lengthy && p.cols < 256)
+    parts = std::max<int64_t>(1, std::min((B > 1 ? 2 * kSlots : kSlots) / blocks_of(p.cols), expect / kLeast));
   const int64_t each = (max_len + parts - 1) / parts;
   p.chunk = (each + 63) / 64 * 64;
   p.parts = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
@@ -639,7 +751,8 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
 }
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t st) {
-  const PromptPlan p = prompt_plan(a.T, a.B, a.Hq, a.Hk, a.D, a.max_len);
+  PromptPlan p = prompt_plan(a.T, a.B, a.Hq, a.Hk, a.D, a.max_len, a.kv != PromptKv::kDense);
+  if (a.kv == PromptKv::kPagedFp8 && p.cols == 256) p.cols = 128, p.tiles = a.T * (a.Hq / a.Hk) / 128 + std::min<int64_t>(a.B, a.T);
   switch (a.kv) {
     case PromptKv::kDense: return launch_kv<PromptKv::kDense>(a, p, st);
     case PromptKv::kPagedBf16: return launch_kv<PromptKv::kPagedBf16>(a, p, st);
