@@ -116,7 +116,7 @@ struct PromptPlan {
   int64_t tiles, chunk;
 };
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged);
-hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t st);
+hipError_t launch_prompt_attention(const PromptArgs& a, PromptPlan p, hipStream_t st);
 
 }  // namespace jq
 

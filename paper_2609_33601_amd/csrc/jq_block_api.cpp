@@ -108,35 +108,37 @@ size_t attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, 
   return round_up(rows * (static_cast<size_t>(D) + 2) * sizeof(float), kWsAlign);
 }
 
-// Sizes of jq_prompt_attention and jq_chunk_attention.
-jq_status check_prompt(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
+// Sizes of jq_prompt_attention and jq_chunk_attention, and how such a call is cut.
+jq_status plan_prompt(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged, jq::PromptPlan* p) {
   if (T <= 0 || B <= 0 || Hq <= 0 || Hk <= 0 || max_len <= 0) return JQ_ERR_INVALID_ARG;
   if (Hq % Hk != 0 || (D != 64 && D != 128 && D != 256)) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (T > kMaxAxis || max_len > kMaxAxis || B > (1 << 20) || Hq > 65536) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (T * Hq >= (int64_t(1) << 31)) return JQ_ERR_UNSUPPORTED_SHAPE;
-  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len, paged);
+  *p = jq::prompt_plan(T, B, Hq, Hk, D, max_len, paged);
   // grids of fewer than 2^24 blocks of 256 threads (an 8-bit cache takes 128 columns where others take 256)
-  return (p.cols == 256 ? 2 : 1) * p.tiles * Hk * p.parts < kMaxBlocks ? JQ_OK : JQ_ERR_UNSUPPORTED_SHAPE;
+  return (p->cols == 256 ? 2 : 1) * p->tiles * Hk * p->parts < kMaxBlocks ? JQ_OK : JQ_ERR_UNSUPPORTED_SHAPE;
 }
 
-size_t prompt_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
-  if (check_prompt(T, B, Hq, Hk, D, max_len, paged) != JQ_OK) return 0;
-  const jq::PromptPlan p = jq::prompt_plan(T, B, Hq, Hk, D, max_len, paged);
+size_t prompt_workspace(int64_t T, int64_t Hq, int64_t D, const jq::PromptPlan& p) {
   if (p.parts == 1) return 0;
   const size_t rows = static_cast<size_t>(T) * static_cast<size_t>(Hq) * p.parts;
   return round_up(rows * (static_cast<size_t>(D) + 2) * sizeof(float), kWsAlign);
+}
+size_t prompt_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
+  jq::PromptPlan p;
+  return plan_prompt(T, B, Hq, Hk, D, max_len, paged, &p) == JQ_OK ? prompt_workspace(T, Hq, D, p) : 0;
 }
 
 // What the two calls share: the queries, their starts, outputs and workspace.
 jq_status check_prompt_call(const void* q, int64_t q_stride, const int32_t* starts, int64_t T, int64_t B, int64_t Hq,
                             int64_t Hk, int64_t D, int64_t max_len, bool paged, const void* out, const float* lse,
-                            const void* workspace, size_t workspace_bytes) {
+                            const void* workspace, size_t workspace_bytes, jq::PromptPlan* p) {
   if (q == nullptr || starts == nullptr || out == nullptr) return JQ_ERR_INVALID_ARG;
-  jq_status st = check_prompt(T, B, Hq, Hk, D, max_len, paged);
+  jq_status st = plan_prompt(T, B, Hq, Hk, D, max_len, paged, p);
   if (st == JQ_OK) st = check_stride(q_stride, Hq * D);
   if (st != JQ_OK) return st;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(starts, 4) || !aligned(lse, 4)) return JQ_ERR_MISALIGNED;
-  const size_t need = prompt_workspace_bytes(T, B, Hq, Hk, D, max_len, paged);
+  const size_t need = prompt_workspace(T, Hq, D, *p);
   if (need > 0) {
     if (workspace == nullptr) return JQ_ERR_INVALID_ARG;
     if (!aligned(workspace, kWsAlign)) return JQ_ERR_MISALIGNED;
@@ -377,7 +379,8 @@ jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, in
                               int64_t B, int64_t Hq, int64_t Hk, int64_t D, float sm_scale, int causal, void* out,
                               float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (k == nullptr || v == nullptr) return JQ_ERR_INVALID_ARG;
-  jq_status st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, Tk, false, out, lse, workspace, workspace_bytes);
+  jq::PromptPlan plan;
+  jq_status st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, Tk, false, out, lse, workspace, workspace_bytes, &plan);
   if (st == JQ_OK) st = check_key_stride(k_stride, Hk * D);
   if (st == JQ_OK) st = check_key_stride(v_stride, Hk * D);
   if (st != JQ_OK) return st;
@@ -389,7 +392,7 @@ jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, in
   a.T = T, a.Tk = Tk, a.B = static_cast<int>(B), a.Hq = static_cast<int>(Hq), a.Hk = static_cast<int>(Hk);
   a.D = static_cast<int>(D), a.max_len = static_cast<int>(Tk), a.scale = sm_scale, a.causal = causal != 0;
   a.kv = jq::PromptKv::kDense;
-  return from_hip(jq::launch_prompt_attention(a, as_stream(stream)));
+  return from_hip(jq::launch_prompt_attention(a, plan, as_stream(stream)));
 }
 
 size_t jq_chunk_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len) {
@@ -404,7 +407,9 @@ jq_status jq_chunk_attention(const void* q, int64_t q_stride, const void* k_cach
                              size_t workspace_bytes, void* stream) {
   if (page_table == nullptr || lens == nullptr || table_cols <= 0) return JQ_ERR_INVALID_ARG;
   jq_status st = check_cache(Hk, k_cache, v_cache, k_scale, v_scale, num_pages, page_size, type);
-  if (st == JQ_OK) st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, max_len, true, out, lse, workspace, workspace_bytes);
+  jq::PromptPlan plan;
+  if (st == JQ_OK)
+    st = check_prompt_call(q, q_stride, starts, T, B, Hq, Hk, D, max_len, true, out, lse, workspace, workspace_bytes, &plan);
   if (st != JQ_OK) return st;
   if (table_cols > kMaxAxis) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (max_len > table_cols * page_size) return JQ_ERR_INVALID_ARG;
@@ -417,7 +422,7 @@ jq_status jq_chunk_attention(const void* q, int64_t q_stride, const void* k_cach
   a.D = static_cast<int>(D), a.page_shift = page_shift(page_size), a.max_len = static_cast<int>(max_len);
   a.scale = sm_scale, a.causal = causal != 0;
   a.kv = type == JQ_CACHE_FP8 ? jq::PromptKv::kPagedFp8 : jq::PromptKv::kPagedBf16;
-  return from_hip(jq::launch_prompt_attention(a, as_stream(stream)));
+  return from_hip(jq::launch_prompt_attention(a, plan, as_stream(stream)));
 }
 
 }  // extern "C"

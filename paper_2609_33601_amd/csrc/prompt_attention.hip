@@ -126,10 +126,49 @@ struct Sizes {
   static constexpr int kHalf = kKeys * kRow;        // a step's keys, or its values
   static constexpr int kStage = 2 * kHalf + (KV == PromptKv::kPagedFp8 ? 8 * kKeys : 0);
   static constexpr int kLane = QG * (D / 2 + 2);    // floats of a lane's result: outputs, maxima, sums
-  static constexpr int kJoin = 2 * 64 * 4 * kLane + 16;  // two waves' results, where halves of the keys are joined
+  static constexpr int kJoin = 2 * 64 * 4 * kLane;  // two waves' results, where halves of the keys are joined
   static constexpr int kLds = 2 * kStage > kJoin ? 2 * kStage : kJoin;
   static constexpr int kPerSimd = D <= 128 ? 2 : 1;
+  // Two steps at a time, with their buffers at constant places, where registers
+  // allow (8192 tokens, 32 heads of 128: 1050 -> 1036 us; 4096, 16 heads of 256,
+  // causal: 198 -> 187).
+  static constexpr bool kUnroll = QG == 1 && !(D == 256 && KV == PromptKv::kPagedFp8);
 };
+
+// The place of a key's (or value's) row: its first element, and the index of its scale.
+template <int D, PromptKv KV>
+__device__ __forceinline__ int64_t row_place(const PromptArgs& a, int seq, int hk, int key0, int t, int64_t stride,
+                                             int64_t* line) {
+  if constexpr (KV == PromptKv::kDense) {
+    return static_cast<int64_t>(key0 + t) * stride + static_cast<int64_t>(hk) * D;
+  } else {
+    const uint32_t pg = static_cast<uint32_t>(a.table[static_cast<int64_t>(seq) * a.table_cols + (t >> a.page_shift)]);
+    const int64_t page = pg < static_cast<uint32_t>(a.num_pages) ? pg : 0;
+    *line = ((page * a.Hk + hk) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
+    return *line * D;
+  }
+}
+template <PromptKv KV>
+__device__ __forceinline__ float one_value(const void* p, int64_t i) {
+  if constexpr (KV == PromptKv::kPagedFp8) {
+    const uint32_t u = static_cast<const uint8_t*>(p)[i];
+    return bf_lo(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, false)) & 0xFFFFu);
+  } else {
+    return bf_lo(static_cast<const uint16_t*>(p)[i]);
+  }
+}
+
+// Whether any value of the tokens [t0, t1) is an infinity or NaN; for one wave.
+template <int D, PromptKv KV>
+__device__ __forceinline__ bool odd_values(const PromptArgs& a, int seq, int hk, int key0, int t0, int t1) {
+  float sum = 0.0f;
+  for (int t = t0 + (threadIdx.x & 63); t < t1; t += 64) {
+    int64_t line;
+    const int64_t at = row_place<D, KV>(a, seq, hk, key0, t, a.v_stride, &line);
+    for (int d = 0; d < D; ++d) sum = fmaf(one_value<KV>(a.v, at + d), 0.0f, sum);
+  }
+  return __any(sum != 0.0f) != 0;
+}
 
 // One column's keys [t0, t1) by one wave, in fp32 and straight from memory: for
 // columns beside which a product met an infinity or NaN among the values of
@@ -143,25 +182,7 @@ __device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int tok
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63;
   const uint16_t* q = a.q + static_cast<int64_t>(token) * a.q_stride + static_cast<int64_t>(head) * D;
-  // a key's (or value's) place: element offset of its row, and index of its scale
-  auto place = [&](int t, int64_t stride, int64_t* line) {
-    if constexpr (KV == PromptKv::kDense) {
-      return static_cast<int64_t>(key0 + t) * stride + static_cast<int64_t>(hk) * D;
-    } else {
-      const uint32_t pg = static_cast<uint32_t>(a.table[static_cast<int64_t>(seq) * a.table_cols + (t >> a.page_shift)]);
-      const int64_t page = pg < static_cast<uint32_t>(a.num_pages) ? pg : 0;
-      *line = ((page * a.Hk + hk) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
-      return *line * D;
-    }
-  };
-  auto value = [](const void* p, int64_t i) {
-    if constexpr (KV == PromptKv::kPagedFp8) {
-      const uint32_t u = static_cast<const uint8_t*>(p)[i];
-      return bf_lo(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, false)) & 0xFFFFu);
-    } else {
-      return bf_lo(static_cast<const uint16_t*>(p)[i]);
-    }
-  };
+  auto place = [&](int t, int64_t stride, int64_t* line) { return row_place<D, KV>(a, seq, hk, key0, t, stride, line); };
   const float scale2 = power_scale(a.scale), sign = a.scale < 0.0f ? -1.0f : 1.0f;
   float m = kNegInf, l = 0.0f, acc[kPer];
 #pragma unroll
@@ -172,7 +193,7 @@ __device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int tok
     if (t + lane < t1) {
       const int64_t at = place(t + lane, a.k_stride, &line);
       float dot = 0.0f;
-      for (int d = 0; d < D; ++d) dot = fmaf(bf_lo(q[d]), value(a.k, at + d), dot);
+      for (int d = 0; d < D; ++d) dot = fmaf(bf_lo(q[d]), one_value<KV>(a.k, at + d), dot);
       if constexpr (KV == PromptKv::kPagedFp8) dot *= a.k_scale[line];
       s = sign * dot * scale2;
     }
@@ -193,7 +214,7 @@ __device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int tok
       float w = __shfl(p, i, 64);
       if constexpr (KV == PromptKv::kPagedFp8) w *= a.v_scale[line];
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) acc[j] = fmaf(w, value(a.v, at + lane * kPer + j), acc[j]);
+      for (int j = 0; j < kPer; ++j) acc[j] = fmaf(w, one_value<KV>(a.v, at + lane * kPer + j), acc[j]);
     }
   }
   if (bad) l = __builtin_nanf("");
@@ -391,7 +412,6 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
-  bool leaked = false;
   // The keys t0 .. of a stage: all of them, or half `part` of them.
   auto step = [&](const uint8_t* stage, int t0, int part, auto count, auto mask) __attribute__((always_inline)) {
     constexpr int kSub = decltype(count)::value;
@@ -489,17 +509,6 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         for (int j = 0; j < 8; ++j) e[j] = s[k16 / 2][g][8 * (k16 & 1) + j];
         p[k16][g] = __builtin_bit_cast(bf16x8, pack8_bf16(e));
       }
-    if (kMask && a.causal) {
-      // An infinity or NaN among these values reaches, through a weight of 0,
-      // also columns that do not see its token.
-      uint32_t hit = 0;
-      for (int i = lane; i < 2 * kSub * Z::kRow; i += 64) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(base + Z::kHalf + 16 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) hit |= (v[j] & 0x7FFF7FFFu) + 0x00800080u;
-      }
-      leaked |= __any((hit & 0x80008000u) != 0) != 0;
-    }
 #pragma unroll
     for (int k16 = 0; k16 < 2 * kSub; ++k16)
 #pragma unroll
@@ -536,9 +545,18 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
     const int plain = busy ? max(min(wave_all, t_end) - first + 64 - 32 * decltype(count)::value, 0) / kKeys : 0;
     const int seen = busy ? max(min(wave_end, t_end) - first + kKeys - 1, 0) / kKeys : 0;
     int i = 0;
-    for (; i < plain; ++i) {
-      arrive(i);
-      step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, part, count, std::false_type());
+    if constexpr (Z::kUnroll) {
+      for (; i + 1 < plain; i += 2) {
+        arrive(i);
+        step(lds, t_begin + i * kKeys, part, count, std::false_type());
+        arrive(i + 1);
+        step(lds + Z::kStage, t_begin + (i + 1) * kKeys, part, count, std::false_type());
+      }
+    } else {
+      for (; i < plain; ++i) {
+        arrive(i);
+        step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, part, count, std::false_type());
+      }
     }
     for (; i < seen; ++i) {
       arrive(i);
@@ -555,7 +573,6 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
     // the second pair's results through LDS to the first
     __syncthreads();
     float* mine = reinterpret_cast<float*>(lds) + (wave & 1) * 64 * Z::kLane;
-    int* flag = reinterpret_cast<int*>(lds + Z::kJoin - 16) + (wave & 1);
     if (wave >= 2) {
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
@@ -568,11 +585,9 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         mine[QG * kOut * 1024 + 128 * g + lane] = m[g];
         mine[QG * kOut * 1024 + 128 * g + 64 + lane] = l[g];
       }
-      if (lane == 0) *flag = leaked;
     }
     __syncthreads();
     if (wave >= 2) return;
-    leaked |= *flag != 0;
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
       const float m1 = mine[QG * kOut * 1024 + 128 * g + lane], l1 = mine[QG * kOut * 1024 + 128 * g + 64 + lane];
@@ -591,6 +606,20 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
     }
   }
   if (!busy) return;
+  // An infinity or NaN among the values of tokens that only some of the columns
+  // see reaches the others through a weight of 0.  Seldom enough to look for
+  // such values only where there is such a result.
+  bool leaked = false;
+  if (a.causal) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < QG; ++g)
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum = fmaf(o[t][g][i], 0.0f, sum);
+    if (__any(sum != 0.0f)) leaked = odd_values<D, KV>(a, at.seq, hk, key0, max(wave_all, t_begin), t_end);
+  }
   if (leaked) {
     for (int i = 0; i < 32 * QG && wcol + i < cols; ++i) {
       const int col = wcol + i, token = col / G;
@@ -733,30 +762,68 @@ hipError_t launch_kv(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
 
 }  // namespace
 
+// What a call takes, in us, from what its blocks' steps took over 71 chunked
+// shapes (1 to 64 sequences, 1 to 1024 new tokens, 600 to 32768 cached, equal
+// and ragged, both caches, every choice of columns and parts timed): a step of
+// 64 keys, alone on a CU or in pairs, for 128 columns and for up to 64, and the
+// join.  The choice by this is 3.4% from the best one on average; a fixed
+// number of blocks a CU was 21%.
+static float prompt_cost(int64_t cols, int64_t blocks, int64_t steps, int64_t parts, int64_t rows, int64_t D, bool half) {
+  constexpr float kAlone[2] = {1.15f, 0.85f}, kPair[2] = {1.84f, 1.11f}, kWhole = 0.6f;
+  const float n = static_cast<float>(blocks * parts);
+  auto rounds = [&](int64_t slots) {
+    return kWhole * static_cast<float>((blocks * parts + slots - 1) / slots) + (1.0f - kWhole) * n / static_cast<float>(slots);
+  };
+  float us;  // of a step, with what waits for a place
+  if (D == 256) us = 2.09f * kAlone[half] * std::max(1.0f, rounds(256));
+  else us = (D == 64 ? 0.77f : 1.0f) * (blocks * parts <= 256 ? kAlone[half] : kPair[half] * std::max(1.0f, rounds(512)));
+  us *= static_cast<float>(steps);
+  if (parts > 1) us += 4.0f + static_cast<float>(rows * parts * (D + 2)) * (8.0f / 5.0e6f);
+  return us;
+}
+
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
-  const int64_t G = Hq / Hk, expect = paged ? max_len : max_len / B;  // keys of a sequence
-  constexpr int64_t kSlots = 512, kLeast = 128;                       // blocks that run at once; keys of a part
-  auto blocks_of = [&](int64_t cols) { return std::max((T * G + cols - 1) / cols, B) * Hk; };
-  const bool lengthy = paged ? max_len >= 512 : expect >= 4096 || (expect >= 512 && max_len >= 4 * T);
+  const int64_t G = Hq / Hk, expect = paged ? max_len : max_len / B + 1;  // keys of a sequence
+  auto blocks_of = [&](int64_t cols) { return std::max((T * G + cols - 1) / cols, std::min(B, T)) * Hk; };
   PromptPlan p;
-  p.cols = D == 64 && T * G / 256 * Hk >= kSlots ? 256 : lengthy || blocks_of(128) >= 384 ? 128 : 64;
+  p.parts = 1;
+  p.chunk = (max_len + 63) / 64 * 64;
+  if (D == 64 && T * G / 256 * Hk >= 512) {
+    // columns enough for blocks of 256, whose waves read a key for 64 columns
+    // instead of 32 (4096 tokens, 32 heads: 167 us with 128, 146 with 256)
+    p.cols = 256;
+  } else {
+    // A prompt over its own keys is not cut: half its parts would see nothing
+    // (1024 tokens, 32 heads on 8 key heads of 128: 21 us, in two parts 35).
+    const bool cut = paged ? max_len >= 256 : expect >= 4096 || (expect >= 512 && max_len >= 4 * T);
+    float best = 0.0f;
+    for (const int cols : {128, 64}) {
+      const int64_t blocks = blocks_of(cols);
+      const bool half = cols == 64 || T * G <= 64 * std::min(B, T);
+      for (int64_t parts = 1; parts <= 256; parts += (parts + 3) / 4) {
+        const int64_t chunk = ((expect + parts - 1) / parts + 63) / 64;  // steps
+        if (parts > 1 && (!cut || chunk < 2)) break;
+        const float us = prompt_cost(cols, blocks, chunk, (expect + 64 * chunk - 1) / (64 * chunk), T * Hq, D, half);
+        if (best == 0.0f || us < best) {
+          best = us;
+          p.cols = cols;
+          p.chunk = parts == 1 ? (max_len + 63) / 64 * 64 : std::max(64 * chunk, (max_len / parts + 63) / 64 * 64);
+        }
+      }
+    }
+    p.parts = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
+  }
   p.tiles = T * G / p.cols + std::min(B, T);  // the most that B sequences of T tokens have
-  int64_t parts = 1;
-  if (lengthy && p.cols < 256)
-    parts = std::max<int64_t>(1, std::min((B > 1 ? 2 * kSlots : kSlots) / blocks_of(p.cols), expect / kLeast));
-  const int64_t each = (max_len + parts - 1) / parts;
-  p.chunk = (each + 63) / 64 * 64;
-  p.parts = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
   return p;
 }
 
-hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t st) {
-  PromptPlan p = prompt_plan(a.T, a.B, a.Hq, a.Hk, a.D, a.max_len, a.kv != PromptKv::kDense);
-  if (a.kv == PromptKv::kPagedFp8 && p.cols == 256) p.cols = 128, p.tiles = a.T * (a.Hq / a.Hk) / 128 + std::min<int64_t>(a.B, a.T);
+hipError_t launch_prompt_attention(const PromptArgs& a, PromptPlan p, hipStream_t st) {
   switch (a.kv) {
     case PromptKv::kDense: return launch_kv<PromptKv::kDense>(a, p, st);
     case PromptKv::kPagedBf16: return launch_kv<PromptKv::kPagedBf16>(a, p, st);
-    default: return launch_kv<PromptKv::kPagedFp8>(a, p, st);
+    default:
+      if (p.cols == 256) p.cols = 128, p.tiles = a.T * (a.Hq / a.Hk) / 128 + std::min<int64_t>(a.B, a.T);
+      return launch_kv<PromptKv::kPagedFp8>(a, p, st);
   }
 }
 

@@ -40,6 +40,8 @@ def attention(q, k, v, causal=True, sm_scale=None):
         a = p @ torch.where(bad[:, None], 0.0, vh.abs())
         for j in bad.nonzero().flatten().tolist():
             o = o + torch.where(seen[:, j, None], p[:, j, None] * vh[j], 0.0)
+            # its weight is rounded too, which moves what its finite values add
+            a = a + p[:, j, None] * torch.where(vh[j].isfinite(), vh[j].abs(), 0.0)
         out[:, h] = torch.where(some[:, None], o, 0.0)
         lse[:, h] = torch.where(some, (top + torch.log(total))[:, 0], -math.inf)
         # a score's error moves every weight, the denominator's too; weights are rounded to bf16 once; the sums'
