@@ -62,7 +62,7 @@ struct AppendArgs {
   // with a norm of each head first, and then also with the keys written
   // densely, and without a cache (k_cache = nullptr)
   const uint16_t *q_weight = nullptr, *k_weight = nullptr;
-  float eps = 0.0f;
+  float eps = 0.0f, inv_d = 0.0f;  // 1 / D
   uint16_t* k_out = nullptr;
   int64_t k_out_stride = 0;
 };

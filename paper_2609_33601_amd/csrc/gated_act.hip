@@ -12,8 +12,8 @@
 //   int4: s = max|y| / 7 per row, q = clamp(rne(y / s), -8, 7), two a byte
 //
 // y stays in fp32 from the loads to the one rounding at the end.  All three are
-// taken through e^-|.|, so the left tail keeps its relative accuracy (1 + erf
-// and 1 + tanh lose it by cancellation).
+// products of positive terms, so the left tail keeps its relative accuracy
+// (1 + erf and 1 + tanh lose it by cancellation).
 //
 // Bound: HBM; each element is read and written once.
 
@@ -31,11 +31,10 @@ using namespace block_detail;
 
 constexpr float kLog2E = 1.44269504088896340736f;
 
-// 1 / (1 + e^-w) times x.
+// x / (1 + 2^-w).  Where 2^-w passes fp32's range the result is next to 0 (below
+// |x| 2^-126) and becomes 0.
 __device__ __forceinline__ float times_logistic(float x, float w) {
-  const float e = __builtin_amdgcn_exp2f(-fabsf(w) * kLog2E);
-  const float r = __builtin_amdgcn_rcpf(1.0f + e);
-  return x * (w < 0.0f ? e * r : r);
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-w));
 }
 
 // Phi(-|x|) = e^(-x^2 / 2) erfcx(z) / 2, z = |x| / sqrt(2); erfcx (e^(z^2)
@@ -60,23 +59,25 @@ __device__ __forceinline__ float times_normal(float x) {
 
 template <Act ACT>
 __device__ __forceinline__ float activate(float x) {
-  if constexpr (ACT == Act::kSilu) return times_logistic(x, x);
+  constexpr float kU = 1.59576912160573071176f * kLog2E;  // 2 sqrt(2 / pi), for a power of two
+  if constexpr (ACT == Act::kSilu) return times_logistic(x, x * kLog2E);
   else if constexpr (ACT == Act::kGelu) return times_normal(x);
-  else return times_logistic(x, 1.59576912160573071176f * fmaf(0.044715f * x * x, x, x));
+  else return times_logistic(x, x * fmaf(x * x, 0.044715f * kU, kU));
 }
 
 // y of 8 elements.
 template <Act ACT, bool GATED>
-__device__ __forceinline__ void load_y(const ActArgs& a, int64_t row, int k, float* y) {
-  unpack8_bf16(*reinterpret_cast<const u32x4*>(a.gate + row * a.gate_stride + k), y);
+__device__ __forceinline__ void apply(u32x4 gate, u32x4 up, float* y) {
+  unpack8_bf16(gate, y);
   float u[8];
-  if constexpr (GATED) unpack8_bf16(*reinterpret_cast<const u32x4*>(a.up + row * a.up_stride + k), u);
+  if constexpr (GATED) unpack8_bf16(up, u);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     y[j] = activate<ACT>(y[j]);
     if constexpr (GATED) y[j] *= u[j];
   }
 }
+__device__ __forceinline__ u32x4 load8(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
 
 __device__ __forceinline__ uint32_t max8(const float* y) {
   uint32_t m = 0;
@@ -85,30 +86,44 @@ __device__ __forceinline__ uint32_t max8(const float* y) {
   return m;
 }
 
-// bf16 and fp8: a wave takes 512 columns of a row.
-template <Act ACT, bool GATED, bool FP8>
+// bf16 and fp8: a wave takes NC chunks of 512 columns of a row.
+template <Act ACT, bool GATED, bool FP8, int NC>
 __global__ __launch_bounds__(256) void gated_act_kernel(const ActArgs a) {
   const int lane = threadIdx.x & 63;
-  const uint32_t per_row = (static_cast<uint32_t>(a.N) + 511) / 512;
+  const uint32_t per_row = (static_cast<uint32_t>(a.N) + 512 * NC - 1) / (512 * NC);
   const uint32_t units = static_cast<uint32_t>(a.M) * per_row;
   // every lane stays to the end: a block's maximum is of 16 lanes
   for (uint32_t u = blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += gridDim.x * 4) {
     const uint32_t row = u / per_row;
-    const int k = static_cast<int>(u - row * per_row) * 512 + lane * 8;
-    const bool in = k < a.N;
-    float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (in) load_y<ACT, GATED>(a, row, k, y);
-    const int64_t at = static_cast<int64_t>(row) * a.N + k;
-    if constexpr (FP8) {
-      const float s = e4m3_scale(lanes_max<16>(max8(y)));
-      const E4m3Divisor d = e4m3_divisor(s);
-      if (!in) continue;
+    const int k0 = static_cast<int>(u - row * per_row) * 512 * NC + lane * 8;
+    u32x4 gate[NC], up[NC];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = e4m3_quotient(y[j], d);
-      *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.y) + at) = pack8_e4m3(y);
-      if (k % 128 == 0) a.scale[static_cast<int64_t>(row) * ((a.N + 127) / 128) + k / 128] = s;
-    } else {
-      if (in) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + at) = pack8_bf16(y);
+    for (int c = 0; c < NC; ++c) {
+      const int k = k0 + 512 * c;
+      gate[c] = up[c] = u32x4{0, 0, 0, 0};
+      if (k < a.N) {
+        gate[c] = load8(a.gate + row * a.gate_stride + k);
+        if constexpr (GATED) up[c] = load8(a.up + row * a.up_stride + k);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int k = k0 + 512 * c;
+      const bool in = k < a.N;
+      float y[8];
+      apply<ACT, GATED>(gate[c], up[c], y);
+      const int64_t at = static_cast<int64_t>(row) * a.N + k;
+      if constexpr (FP8) {
+        const float s = e4m3_scale(lanes_max<16>(max8(y)));
+        const E4m3Divisor d = e4m3_divisor(s);
+        if (!in) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = e4m3_quotient(y[j], d);
+        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.y) + at) = pack8_e4m3(y);
+        if (k % 128 == 0) a.scale[static_cast<int64_t>(row) * ((a.N + 127) / 128) + k / 128] = s;
+      } else {
+        if (in) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.y) + at) = pack8_bf16(y);
+      }
     }
   }
 }
@@ -126,7 +141,8 @@ __global__ __launch_bounds__(1024) void gated_act_int4_kernel(const ActArgs a) {
       const int k = (c * waves + wave) * 512 + lane * 8;
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[c][j] = 0.0f;
-      if (k < a.N) load_y<ACT, GATED>(a, row, k, y[c]);
+      if (k < a.N)
+        apply<ACT, GATED>(load8(a.gate + row * a.gate_stride + k), GATED ? load8(a.up + row * a.up_stride + k) : u32x4{}, y[c]);
       m = umax(m, max8(y[c]));
     }
     m = wave_max_bits(m);
@@ -150,10 +166,14 @@ template <Act ACT, bool GATED>
 hipError_t launch(const ActArgs& a, NormOut out, hipStream_t st) {
   constexpr int64_t kMostBlocks = 1 << 20;
   if (out != NormOut::kInt4) {
-    const int64_t blocks = (a.M * ((a.N + 511) / 512) + 3) / 4;
+    // With an up a wave has as much on its way with one chunk (8192 x 12288 to
+    // e4m3 91 us with one and with two, 2747 x 2816 to bf16 10.8 and 11.5) as
+    // without one with two (4608 x 12288 to e4m3 42 and 38.6).
+    constexpr int kChunks = GATED ? 1 : 2;
+    const int64_t blocks = (a.M * ((a.N + 512 * kChunks - 1) / (512 * kChunks)) + 3) / 4;
     const dim3 grid(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
-    if (out == NormOut::kFp8) hipLaunchKernelGGL((gated_act_kernel<ACT, GATED, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((gated_act_kernel<ACT, GATED, false>), grid, dim3(256), 0, st, a);
+    if (out == NormOut::kFp8) hipLaunchKernelGGL((gated_act_kernel<ACT, GATED, true, kChunks>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((gated_act_kernel<ACT, GATED, false, kChunks>), grid, dim3(256), 0, st, a);
   } else {
     const int chunks = (a.N + 511) / 512;
     const dim3 grid(static_cast<unsigned>(a.M < kMostBlocks ? a.M : kMostBlocks));

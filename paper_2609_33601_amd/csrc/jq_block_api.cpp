@@ -346,7 +346,7 @@ jq_status jq_qk_norm_rope_append(const void* q, int64_t q_stride, const void* k,
     a.page = static_cast<int>(page_size), a.page_shift = page_shift(page_size);
     a.fp8 = type == JQ_CACHE_FP8;
   }
-  a.q_weight = u16(q_weight), a.k_weight = u16(k_weight), a.eps = eps;
+  a.q_weight = u16(q_weight), a.k_weight = u16(k_weight), a.eps = eps, a.inv_d = 1.0f / static_cast<float>(D);
   a.k_out = static_cast<uint16_t*>(k_out), a.k_out_stride = k_out_stride;
   return from_hip(jq::launch_norm_rope_append(a, as_stream(stream)));
 }

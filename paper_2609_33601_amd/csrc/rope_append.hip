@@ -66,7 +66,25 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
     float f[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) f[j] = 0.0f;
+    u32x4 w0 = {0, 0, 0, 0}, w1 = {0, 0, 0, 0};
+    float cs[8], sn[8];
+    if (live && turned) {
+      // a position outside the tables has no rotation: NaN
+      const int64_t row = (pos_ok ? pos : 0) * half + 8 * c;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        *reinterpret_cast<f32x4*>(cs + 4 * j) = *reinterpret_cast<const f32x4*>(a.cos + row + 4 * j);
+        *reinterpret_cast<f32x4*>(sn + 4 * j) = *reinterpret_cast<const f32x4*>(a.sin + row + 4 * j);
+      }
+    }
     if (live) {
+      if constexpr (NORM) {
+        if (!is_v) {
+          const uint16_t* weight = is_q ? a.q_weight : a.k_weight;
+          w0 = *reinterpret_cast<const u32x4*>(weight + i0);
+          w1 = *reinterpret_cast<const u32x4*>(weight + i1);
+        }
+      }
       unpack8_bf16(*reinterpret_cast<const u32x4*>(src + i0), f);
       unpack8_bf16(*reinterpret_cast<const u32x4*>(src + i1), f + 8);
     }
@@ -75,26 +93,19 @@ __global__ __launch_bounds__(256) void rope_append_kernel(const AppendArgs a) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) ss = fmaf(f[j], f[j], ss);
       ss = head_sum<LPH>(ss);  // all lanes of the wave take part
-      const float r = 1.0f / sqrtf(ss / static_cast<float>(a.D) + a.eps);
+      const float mean = fmaf(ss, a.inv_d, a.eps);
+      float r = __builtin_amdgcn_rsqf(mean);  // 1 ulp, of what is no subnormal
+      if (mean < 0x1p-120f) r = 1.0f / sqrtf(mean);
       if (live && !is_v) {
-        const uint16_t* weight = is_q ? a.q_weight : a.k_weight;
         float w[16];
-        unpack8_bf16(*reinterpret_cast<const u32x4*>(weight + i0), w);
-        unpack8_bf16(*reinterpret_cast<const u32x4*>(weight + i1), w + 8);
+        unpack8_bf16(w0, w);
+        unpack8_bf16(w1, w + 8);
 #pragma unroll
         for (int j = 0; j < 16; ++j) f[j] = (f[j] * r) * w[j];
       }
     }
     if (live) {
       if (turned) {
-        // a position outside the tables has no rotation: NaN
-        const int64_t row = (pos_ok ? pos : 0) * half + 8 * c;
-        float cs[8], sn[8];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          *reinterpret_cast<f32x4*>(cs + 4 * j) = *reinterpret_cast<const f32x4*>(a.cos + row + 4 * j);
-          *reinterpret_cast<f32x4*>(sn + 4 * j) = *reinterpret_cast<const f32x4*>(a.sin + row + 4 * j);
-        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int ia = INTERLEAVED ? 2 * j : j, ib = INTERLEAVED ? 2 * j + 1 : 8 + j;
