@@ -1,8 +1,9 @@
 """A small decoder served with the library's operators: prompts of different
-lengths go through one causal pass, then every sequence gets new tokens, one at
-a time (or a block at a time, as block diffusion decodes), from a replayed HIP graph.
+lengths go through one causal pass, packed (or a chunk of each at a time), then
+every sequence gets new tokens, one at a time (or a block at a time, as block
+diffusion decodes), from a replayed HIP graph.
 
-    python -m examples.decode [--batch 8] [--prompt 500] [--new 32] [--block 1] [--cache fp8]
+    python -m examples.decode [--batch 8] [--prompt 500] [--chunk 0] [--new 32] [--block 1] [--cache fp8]
 
 Weights are random and the embedding of the next token is the block's last
 output, so what it shows is the operators at work and what they take, not text.
@@ -10,10 +11,10 @@ output, so what it shows is the operators at work and what they take, not text.
 A layer, on rows of tokens with the residual stream r:
 
     h, r = norm(x, r) as int4        -> W4A4 product: q, k, v
-    rotate q and k, append k and v to the paged cache
-    attention over the cache         -> W4A4 linear
+    (norm each head of q and k,) rotate q and k, append k and v to the paged cache
+    attention over the cache, or the packed prompts' own keys -> W4A4 linear
     h, r = norm(., r) as e4m3        -> 8-bit product: gate, up
-    silu(gate) * up                  -> 8-bit linear
+    silu(gate) * up                  -> 8-bit linear (as e4m3 at once, with `fused`)
 """
 
 import argparse
@@ -38,6 +39,8 @@ class Config:
     page: int = 16
     base: float = 10000.0
     cache: str = "fp8"  # or "bf16"
+    head_norm: bool = False  # an RMS norm of each head of q and k before the rotation
+    fused: bool = False  # the gated activation written as the 8-bit product's codes
 
 
 class Layer:
@@ -51,6 +54,8 @@ class Layer:
             "gate_up": randn(2 * c.ffn, c.dim), "down": randn(c.dim, c.ffn, 0.5),
         }
         self.norms = [(1 + 0.1 * torch.randn((c.dim,), generator=gen, device="cuda")).bfloat16() for _ in range(2)]
+        self.head_norms = [(1 + 0.1 * torch.randn((c.head_dim,), generator=gen, device="cuda")).bfloat16()
+                           for _ in range(2)] if c.head_norm else None
         self.qkv, self.o = (jq.jq_pack_weight_int4(self.plain[n]) for n in ("qkv", "o"))
         self.gate_up, self.down = (jb.jq_pack_weight_fp8(self.plain[n]) for n in ("gate_up", "down"))
 
@@ -85,19 +90,27 @@ class Decoder:
         angle = torch.arange(max_tokens, device="cuda", dtype=torch.float64)[:, None] * freq
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
 
-    def forward(self, x, positions, slots, attend, cache):
-        """x bf16 [T,dim], the new tokens of all sequences; attend(layer, q [T,heads,head_dim]) is their attention."""
+    def forward(self, x, positions, slots, attend, cache, dense=False):
+        """x bf16 [T,dim], the new tokens of all sequences; attend(layer, q [T,heads,head_dim], k, v) is their attention
+        (k, rotated, only if `dense`, which takes head norms; else None)."""
         c, T = self.c, x.shape[0]
         r = torch.zeros_like(x)
         for i, layer in enumerate(self.layers):
             q4, s4, r = jb.jq_rmsnorm(x, layer.norms[0], residual=r, out="int4")
             qkv = jq.jq_w4a4_gemm(q4, s4, *layer.qkv).view(T, c.heads + 2 * c.key_heads, c.head_dim)
             q, k, v = qkv.split((c.heads, c.key_heads, c.key_heads), dim=1)
-            q = jb.jq_rope_append(q, k, v, positions, self.cos, self.sin, slots, *cache.kv[i], *cache.scales[i])
-            x = jq.jq_w4a4_linear(attend(i, q).reshape(T, -1), *layer.o)
+            where = (positions, self.cos, self.sin, slots, *cache.kv[i], *cache.scales[i])
+            if c.head_norm:
+                q, k = jb.jq_qk_norm_rope_append(q, k, v, *layer.head_norms, *where, dense_k=dense)
+            else:
+                q, k = jb.jq_rope_append(q, k, v, *where), None
+            x = jq.jq_w4a4_linear(attend(i, q, k, v).reshape(T, -1), *layer.o)
             q8, s8, r = jb.jq_rmsnorm(x, layer.norms[1], residual=r, out="fp8")
             gate, up = jb.jq_fp8_gemm(q8, s8, *layer.gate_up).chunk(2, dim=1)
-            x = jb.jq_fp8_linear(F.silu(gate) * up, *layer.down)
+            if c.fused:
+                x = jb.jq_fp8_gemm(*jb.jq_gated_act(gate, up, out="fp8"), *layer.down)
+            else:
+                x = jb.jq_fp8_linear(F.silu(gate) * up, *layer.down)
         return jb.jq_rmsnorm(x, self.final, residual=r)[0]
 
     def prefill(self, prompts, cache):
@@ -109,11 +122,34 @@ class Decoder:
             cache.lens[b] = n
             lens, table = cache.lens[b:b + 1], cache.table[b:b + 1]
 
-            def attend(i, q):
+            def attend(i, q, k, v):
                 return jb.jq_paged_attention(q[None], *cache.kv[i], table, lens, *cache.scales[i], max_len=n)[0]
 
             last.append(self.forward(x, at, cache.slots(b, at), attend, cache)[-1])
         return torch.stack(last)
+
+    def extend(self, chunks, cache):
+        """A chunk bf16 [n,dim] (n may be 0) of new tokens of each sequence, packed into one causal pass: prompts, parts of
+        prompts and single tokens side by side.  Returns each chunk's last output, [batch,dim] (0 for an empty one)."""
+        c, new = self.c, [x.shape[0] for x in chunks]
+        before = cache.lens.tolist()
+        sequences = torch.repeat_interleave(torch.arange(len(new)), torch.tensor(new)).cuda()
+        starts = torch.tensor([0] + new).cumsum(0).int()
+        ends = starts[1:].long() - 1
+        at = torch.cat([torch.arange(m, m + n, dtype=torch.int32) for n, m in zip(new, before)]).cuda()
+        starts = starts.cuda()
+        cache.lens += torch.tensor(new, dtype=torch.int32).cuda()
+        # prompts from their first token on see their own keys alone, as they come out of the rotation
+        dense, max_len = c.head_norm and not any(before), max(n + m for n, m in zip(new, before))
+
+        def attend(i, q, k, v):
+            if dense:
+                return jb.jq_prompt_attention(q, k, v, starts)
+            return jb.jq_chunk_attention(q, *cache.kv[i], cache.table, starts, cache.lens, *cache.scales[i],
+                                         max_len=max_len)
+
+        y = self.forward(torch.cat(chunks), at, cache.slots(sequences, at), attend, cache, dense)
+        return torch.where(torch.tensor(new)[:, None].cuda() > 0, y[ends.clamp_min(0).cuda()], 0.0).to(y.dtype)
 
     def step(self, x, cache, max_len):
         """Appends a block x bf16 [batch,n,dim] to every sequence and returns its output; a block sees all of itself.
@@ -124,7 +160,7 @@ class Decoder:
         slots = cache.slots(sequences, positions)
         cache.lens += n
 
-        def attend(i, q):
+        def attend(i, q, k, v):
             return jb.jq_paged_attention(q.view(B, n, *q.shape[1:]), *cache.kv[i], cache.table, cache.lens,
                                          *cache.scales[i], max_len=max_len, causal=False)
 
@@ -150,18 +186,23 @@ def main():
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     p.add_argument("--batch", type=int, default=8)
     p.add_argument("--prompt", type=int, default=500, help="longest prompt; the others are shorter")
+    p.add_argument("--chunk", type=int, default=0, help="tokens of a prompt at a time (0: all of them)")
     p.add_argument("--new", type=int, default=32, help="steps")
     p.add_argument("--block", type=int, default=1, help="tokens of a step")
     p.add_argument("--cache", choices=("fp8", "bf16"), default="fp8")
     a = p.parse_args()
-    c = Config(cache=a.cache)
+    c = Config(cache=a.cache, head_norm=True, fused=True)
     tokens = a.prompt + (a.new + 1) * a.block
     decoder, cache = Decoder(c, tokens), Cache(c, a.batch, tokens)
     prompts = [torch.randn((max(1, a.prompt - 37 * b), c.dim), device="cuda").bfloat16() for b in range(a.batch)]
 
     torch.cuda.synchronize()
     t = time.perf_counter()
-    last = decoder.prefill(prompts, cache)
+    chunk = a.chunk or a.prompt
+    last = torch.zeros((a.batch, c.dim), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, a.prompt, chunk):
+        y = decoder.extend([x[i: i + chunk] for x in prompts], cache)
+        last = torch.where(torch.tensor([[i < len(x)] for x in prompts], device="cuda"), y, last)
     torch.cuda.synchronize()
     print(f"prompts: {sum(len(x) for x in prompts)} tokens in {1e3 * (time.perf_counter() - t):.2f} ms (first calls)")
 
