@@ -255,7 +255,7 @@ size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int
  *   lse          out  [T,Hq] fp32 log of the softmax's denominator (natural
  *                     logarithm, with the maximum in it), or NULL
  *   workspace    at least jq_prompt_attention_workspace_bytes, 256-byte aligned
- *                     (NULL where that is 0)
+ *                     (NULL where that is 0), the call's own until it has run
  * Rows of out and lse before starts[0] and from starts[B] on stay as they are.
  * Starts out of range count as the nearest in range and a sequence that would
  * end before it begins as empty; where they decrease, what the rows hold is
@@ -263,7 +263,7 @@ size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int
  * An infinity or NaN among a token's values reaches the queries that see the
  * token, and no other; a score of -infinity is a weight of 0.  The weights are
  * rounded to bf16 for the product with the values; scores, statistics and sums are fp32.
- * D = 64, 128 or 256; Hq % Hk == 0; T, Tk <= 2^30, B <= 2^20, T * Hq < 2^31 and
+ * D = 64, 128 or 256; Hq % Hk == 0; T, Tk <= 2^30, B <= 65536, T * Hq < 2^31 and
  * fewer than 2^24 blocks (of 128 query columns of a key head and sequence);
  * strides % 8 == 0, at least a token's elements, k_stride and v_stride <= 2^25.
  */

@@ -76,7 +76,7 @@ def test_many_columns(D, Hq, Hk, lens, causal):
     check_all(out, None, q, k, v, lens, lens, causal)
 
 
-@pytest.mark.parametrize("n", [64, 65, 200])
+@pytest.mark.parametrize("n", [64, 65, 200, 257, 700])
 def test_many_sequences(n):
     lens = [(7 * i) % 23 for i in range(n)]
     q, k, v = heads(sum(lens), (4, 2, 2), 64, gen(n))
