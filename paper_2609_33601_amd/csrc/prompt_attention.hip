@@ -538,17 +538,23 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
       if (steps > 1) fetch(t_begin + kKeys);
     } else {
       issue(0, t_begin);
+      if (steps > 1) issue(1, t_begin + kKeys);
     }
   }
   auto arrive = [&](int i) __attribute__((always_inline)) {
-    if constexpr (!kFp8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (i + 1 >= steps) return;
     if constexpr (kFp8) {
+      __syncthreads();
+      if (i + 1 >= steps) return;
       put((i + 1) & 1);
       if (i + 2 < steps) fetch(t_begin + (i + 2) * kKeys);
+    } else if (i == 0 && steps > 1) {
+      // both buffers' transfers are on their way
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+      __syncthreads();
     } else {
-      issue((i + 1) & 1, t_begin + (i + 1) * kKeys);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (i + 1 < steps) issue((i + 1) & 1, t_begin + (i + 1) * kKeys);
     }
   };
   auto run = [&](int part, auto count) __attribute__((always_inline)) {
