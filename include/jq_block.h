@@ -264,7 +264,7 @@ size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int
  * token, and no other; a score of -infinity is a weight of 0.  The weights are
  * rounded to bf16 for the product with the values; scores, statistics and sums are fp32.
  * D = 64, 128 or 256; Hq % Hk == 0; T, Tk <= 2^30, B <= 65536, T * Hq < 2^31 and
- * fewer than 2^24 blocks (of 128 query columns of a key head and sequence);
+ * T * Hq / 128 + 2 * min(B, T) * Hk < 2^24;
  * strides % 8 == 0, at least a token's elements, k_stride and v_stride <= 2^25.
  */
 jq_status jq_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,

@@ -513,6 +513,8 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][g][i]);
       top = max_halves(top) * scale2;
+      // the maximum follows only when left more than 2^8 behind: weights stay
+      // below that, and fp32 sums of them are as exact
       const bool more = top > m[g] + 8.0f;
       if (__any(more)) {
         const float keep = more ? __builtin_amdgcn_exp2f(m[g] - top) : 1.0f;
@@ -824,20 +826,20 @@ hipError_t launch_kv(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
 // number of blocks a CU was 21%.
 static float prompt_cost(int64_t cols, int64_t blocks, int64_t steps, int64_t parts, int64_t rows, int64_t D, bool half) {
   constexpr float kAlone[2] = {1.15f, 0.85f}, kPair[2] = {1.84f, 1.11f}, kWhole = 0.6f;
-  const float n = static_cast<float>(blocks * parts);
+  const float n = static_cast<float>(blocks);
   auto rounds = [&](int64_t slots) {
-    return kWhole * static_cast<float>((blocks * parts + slots - 1) / slots) + (1.0f - kWhole) * n / static_cast<float>(slots);
+    return kWhole * static_cast<float>((blocks + slots - 1) / slots) + (1.0f - kWhole) * n / static_cast<float>(slots);
   };
   float us;  // of a step, with what waits for a place
   if (D == 256) us = 2.09f * kAlone[half] * std::max(1.0f, rounds(256));
-  else us = (D == 64 ? 0.77f : 1.0f) * (blocks * parts <= 256 ? kAlone[half] : kPair[half] * std::max(1.0f, rounds(512)));
+  else us = (D == 64 ? 0.77f : 1.0f) * (blocks <= 256 ? kAlone[half] : kPair[half] * std::max(1.0f, rounds(512)));
   us *= static_cast<float>(steps);
   if (parts > 1) us += 4.0f + static_cast<float>(rows * parts * (D + 2)) * (8.0f / 5.0e6f);
   return us;
 }
 
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
-  const int64_t G = Hq / Hk, expect = paged ? max_len : max_len / B + 1;  // keys of a sequence
+  const int64_t G = Hq / Hk, expect = paged ? max_len : (max_len + B - 1) / B;  // keys of a sequence
   auto blocks_of = [&](int64_t cols) { return std::max((T * G + cols - 1) / cols, std::min(B, T)) * Hk; };
   PromptPlan p;
   p.parts = 1;
@@ -855,13 +857,20 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
       const int64_t blocks = blocks_of(cols);
       const bool half = cols == 64 || T * G <= 64 * std::min(B, T);
       for (int64_t parts = 1; parts <= 256; parts += (parts + 3) / 4) {
-        const int64_t chunk = ((expect + parts - 1) / parts + 63) / 64;  // steps
-        if (parts > 1 && (!cut || chunk < 2)) break;
-        const float us = prompt_cost(cols, blocks, chunk, (expect + 64 * chunk - 1) / (64 * chunk), T * Hq, D, half);
+        // Parts of the longest that a sequence may be; one as long as expected has
+        // `used` of them (8 sequences of 16 on 4096 keys: 59 us uncut, 39 so; 4 of
+        // 77 on 4608, 24 heads: 67 and 56).
+        const int64_t chunk = ((max_len + parts - 1) / parts + 63) / 64;  // steps
+        const int64_t used = (expect + 64 * chunk - 1) / (64 * chunk);
+        if (parts > 1 && (!cut || chunk < 2 || blocks * parts >= 1 << 20)) break;
+        if (parts > 1 && used == 1) continue;
+        const int64_t all = (max_len + 64 * chunk - 1) / (64 * chunk);
+        float us = prompt_cost(cols, blocks * used, std::min(chunk, (expect + 63) / 64), all, T * Hq, D, half);
+        us += 3.0f / 512.0f * static_cast<float>(blocks * (all - used));  // blocks that find nothing to do
         if (best == 0.0f || us < best) {
           best = us;
           p.cols = cols;
-          p.chunk = parts == 1 ? (max_len + 63) / 64 * 64 : std::max(64 * chunk, (max_len / parts + 63) / 64 * 64);
+          p.chunk = 64 * chunk;
         }
       }
     }

@@ -14,7 +14,8 @@
 // and D / 16 lanes hold a head, so the 8-bit cache's maximum is a few DPP
 // steps.  One launch does queries, keys and values.  8191 tokens of 32 + 8 + 8
 // heads of 128 to an 8-bit cache: 36 us, 5.2 TB/s, as plain copies run (0.25 GB
-// 5.4, 4 GB 4.9), and 39 us a call from HBM, 31 from the last-level cache; two, four or eight heads a lane took 41, 43 and 46 us.
+// 5.4, 4 GB 4.9), and 37 us a call from HBM; two, four or eight heads a lane took
+// 41, 43 and 46 us.
 // With the norm, the same tokens returned densely besides (204 MB): 42.7 us, 4.8
 // TB/s; 4608 tokens of 24 + 24 heads without a cache (113 MB): 22.7, 5.1.  What
 // counts there is that the weights and the rotation's rows are asked for with

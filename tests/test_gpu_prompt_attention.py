@@ -66,6 +66,21 @@ def test_keys_apart(lens, klens, D, causal):
     check_all(out, lse, q, k, v, lens, klens, causal)
 
 
+@pytest.mark.parametrize("lens,klens", [([16, 16, 3, 16], [4100, 3000, 0, 2900]), ([1] * 6, [2000, 1, 6500, 63, 64, 1025]),
+                                        ([40, 0, 2], [3001, 500, 1501])], ids=str)
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_keys_apart_in_parts(lens, klens, D, causal):
+    """Several sequences, whose key axes are cut, shorter ones into fewer parts than the longest could have."""
+    Hq, Hk, g = 6, 2, gen(2 * D + sum(klens))
+    assert jb.jq_prompt_attention_workspace_bytes(sum(lens), sum(klens), len(lens), Hq, Hk, D) > 0
+    q, = heads(sum(lens), (Hq,), D, g)
+    k, v = heads(sum(klens), (Hk, Hk), D, g)
+    lse = torch.empty((sum(lens), Hq), device=DEV)
+    out = jb.jq_prompt_attention(q, k, v, starts(lens), starts(klens), causal=causal, lse=lse)
+    check_all(out, lse, q, k, v, lens, klens, causal)
+
+
 @pytest.mark.parametrize("D,Hq,Hk,lens", [(128, 32, 32, [1500, 600]), (128, 32, 8, [2000, 1, 70]), (64, 40, 8, [1700, 130]),
                                           (256, 16, 16, [900, 77])], ids=str)
 @pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
@@ -374,3 +389,39 @@ def test_the_same_call_gives_the_same_bits():
     a = jb.jq_prompt_attention(q, k, v, s)
     for _ in range(3):
         assert torch.equal(jb.jq_prompt_attention(q, k, v, s), a)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_chunk_pages_that_sequences_share(kind):
+    """A common beginning, held once."""
+    g, new, lens = gen(18), [40, 1, 7], [300, 290, 64]
+    kv, scales, table = cache_of(lens, 2, 64, 16, kind, g)
+    table[1, :16] = table[0, :16]
+    table[2, :4] = table[0, 4]
+    q = torch.randn((sum(new), 6, 64), generator=g, device=DEV).bfloat16()
+    out = jb.jq_chunk_attention(q, *kv, table, starts(new), torch.tensor(lens, dtype=torch.int32, device=DEV), *scales)
+    check_chunk(out, None, q, kv, scales, table, new, lens, True)
+
+
+def test_a_graph_follows_its_starts_and_lengths():
+    g, T, cap = gen(19), 96, 2048
+    kv, scales, table = cache_of([cap] * 3, 2, 128, 16, "fp8", g)
+    q = torch.randn((T, 8, 128), generator=g, device=DEV).bfloat16()
+    s, lens = starts([1, 1, 1]), torch.tensor([1, 1, 1], dtype=torch.int32, device=DEV)
+    out = torch.zeros_like(q)
+    call = lambda: jb.jq_chunk_attention(q, *kv, table, s, lens, *scales, max_len=cap, out=out)
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for new, n in (([90, 1, 5], [90, 2048, 700]), ([0, 0, 3], [0, 5, 1999]), ([32, 32, 32], [1000, 31, 64])):
+        s.copy_(starts(new))
+        lens.copy_(torch.tensor(n, dtype=torch.int32))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_chunk(out, None, q, kv, scales, table, new, n, True)
+        assert (out[sum(new):] == 7).all()
+        replayed = out.clone()
+        call()
+        assert torch.equal(out, replayed)
