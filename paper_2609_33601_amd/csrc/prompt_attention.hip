@@ -90,66 +90,71 @@ struct Place {
   int key0, keys;  // rows of its own keys, or cached tokens
 };
 
-// The `index`-th tile of `per` columns, counted from the last one of the last
-// sequence, so that the longest of a causal sequence come first.  All lanes of
-// a wave take part, 64 N sequences at a time (4096 sequences of one token over
-// up to 64, 8 key heads: N = 1 1723 us, 4 970, 16 1222); seq = -1 where there are
-// fewer tiles.  Starts outside [0, T] are brought into it, so whatever they
-// are, the rows lie in the tensors.
+// The rows of sequence b.  Starts outside [0, T] are brought into it, so
+// whatever they are, the rows lie in the tensors.
 __device__ __forceinline__ void rows_of(const int32_t* starts, int64_t T, int b, int* row0, int* rows) {
   const int t = static_cast<int>(T);
   const int s0 = min(max(starts[b], 0), t), s1 = min(max(starts[b + 1], 0), t);
   *row0 = s0;
   *rows = max(s1 - s0, 0);
 }
-template <bool PAGED, int N>
-__device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, int index) {
+
+// The place of the `index`-th of `tiles` tiles of `per` columns, counted from the
+// last one of the last sequence, so that the longest of a causal sequence come
+// first; seq = -1 where there are fewer.  All lanes of a wave take part.
+template <bool PAGED>
+__device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, int index, int tiles) {
   const int lane = threadIdx.x & 63;
-  Place p{-1, 0, 0, 0, 0, 0};
-  int after = 0;  // tiles of the sequences behind
-  for (int base = (a.B - 1) / (64 * N) * (64 * N); base >= 0; base -= 64 * N) {
-    // a lane's N sequences; their keys are asked for with the rows, not after them
-    int row0[N], rows[N], key0[N], keys[N], tiles[N], n = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int b = base + N * lane + i;
-      row0[i] = rows[i] = key0[i] = keys[i] = 0;
-      if (b < a.B) {
-        rows_of(a.starts, a.T, b, &row0[i], &rows[i]);
-        if constexpr (PAGED) keys[i] = min(max(a.lens[b], 0), a.max_len);
-        else rows_of(a.k_starts, a.Tk, b, &key0[i], &keys[i]);
-      }
+  const int shift = __builtin_ctz(per);
+  const bool many = a.B > 64;
+  int first = 0;  // of 64 sequences, a lane each
+  int slot = tiles - 1 - index;
+  if (many) {
+    // Sequence b has the places from starts[b] G / per + b on, as many as it needs
+    // or one more, so a search finds it (4096 sequences of one token over up to
+    // 64, 8 key heads: 350 us, by a walk along all sequences 960).
+    for (int step = a.B > 4096 ? 4096 : 64; step > 1; step /= 64) {
+      const int b = first + lane * step;
+      const int from = b < a.B ? (min(max(a.starts[b], 0), static_cast<int>(a.T)) * G >> shift) + b : slot + 1;
+      const uint64_t hit = __ballot(from <= slot);
+      if (hit == 0) break;  // and below
+      first += (63 - __builtin_clzll(hit)) * step;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) n += tiles[i] = (rows[i] * G + per - 1) / per;
-    int upto = n;  // tiles of this lane's sequences and those behind them, of these 64 N
+  }
+  // a lane's sequence; its keys are asked for with the rows, not after them
+  const int b = first + lane;
+  int row0 = 0, rows = 0, key0 = 0, keys = 0;
+  if (b < a.B) {
+    rows_of(a.starts, a.T, b, &row0, &rows);
+    if constexpr (PAGED) keys = min(max(a.lens[b], 0), a.max_len);
+    else rows_of(a.k_starts, a.Tk, b, &key0, &keys);
+  }
+  const int n = (rows * G + per - 1) >> shift;
+  int tile, l;
+  if (many) {
+    tile = slot - ((row0 * G >> shift) + b);
+    const uint64_t hit = __ballot(b < a.B && tile >= 0);
+    l = hit == 0 ? 0 : 63 - __builtin_clzll(hit);
+  } else {
+    // fewer tiles than places where sequences are empty or fill their last
+    // tile, so without gaps: the sum over the sequences behind
+    int upto = n;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const int v = __shfl_down(upto, d, 64);
       upto += lane + d < 64 ? v : 0;
     }
-    int mine = index - after - (upto - n);  // place among this lane's tiles, from its last
-    const uint64_t hit = __ballot(mine >= 0 && mine < n);
-    if (hit != 0) {
-      const int l = __builtin_ctzll(hit);
-#pragma unroll
-      for (int i = N - 1; i >= 0; --i) {
-        if (p.seq < 0 && mine < tiles[i]) {
-          p = Place{base + N * lane + i, row0[i], rows[i], tiles[i] - 1 - mine, key0[i], keys[i]};
-        } else {
-          mine -= tiles[i];
-        }
-      }
-      p.seq = __builtin_amdgcn_readlane(p.seq, l);
-      p.row0 = __builtin_amdgcn_readlane(p.row0, l);
-      p.rows = __builtin_amdgcn_readlane(p.rows, l);
-      p.tile = __builtin_amdgcn_readlane(p.tile, l);
-      p.key0 = __builtin_amdgcn_readlane(p.key0, l);
-      p.keys = __builtin_amdgcn_readlane(p.keys, l);
-      return p;
-    }
-    after += __builtin_amdgcn_readlane(upto, 0);
+    tile = upto - 1 - index;
+    const uint64_t hit = __ballot(tile >= 0 && tile < n);
+    l = hit == 0 ? 0 : __builtin_ctzll(hit);
   }
+  Place p;
+  p.tile = __builtin_amdgcn_readlane(tile, l);
+  p.seq = p.tile >= 0 && p.tile < __builtin_amdgcn_readlane(n, l) ? first + l : -1;
+  p.row0 = __builtin_amdgcn_readlane(row0, l);
+  p.rows = __builtin_amdgcn_readlane(rows, l);
+  p.key0 = __builtin_amdgcn_readlane(key0, l);
+  p.keys = __builtin_amdgcn_readlane(keys, l);
   return p;
 }
 
@@ -297,7 +302,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
   const int part = rest / tiles;
   const int index = rest % tiles;
-  const Place at = a.B <= 64 ? find_tile<kPaged, 1>(a, G, per, index) : find_tile<kPaged, 4>(a, G, per, index);
+  const Place at = find_tile<kPaged>(a, G, per, index, tiles);
   if (at.seq < 0) return;
 
   const int key0 = at.key0, nk = at.keys;
@@ -838,6 +843,12 @@ static float prompt_cost(int64_t cols, int64_t blocks, int64_t steps, int64_t pa
   return us;
 }
 
+// Places for tiles: the most tiles that B sequences of T tokens have; where they
+// are searched (find_tile), one for each sequence besides the full ones.
+static int64_t prompt_tiles(int64_t T, int64_t B, int64_t G, int64_t cols) {
+  return T * G / cols + (B > 64 ? B : std::min(B, T));
+}
+
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
   const int64_t G = Hq / Hk, expect = paged ? max_len : (max_len + B - 1) / B;  // keys of a sequence
   auto blocks_of = [&](int64_t cols) { return std::max((T * G + cols - 1) / cols, std::min(B, T)) * Hk; };
@@ -876,7 +887,7 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
     }
     p.parts = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
   }
-  p.tiles = T * G / p.cols + std::min(B, T);  // the most that B sequences of T tokens have
+  p.tiles = prompt_tiles(T, B, G, p.cols);
   return p;
 }
 
@@ -885,7 +896,7 @@ hipError_t launch_prompt_attention(const PromptArgs& a, PromptPlan p, hipStream_
     case PromptKv::kDense: return launch_kv<PromptKv::kDense>(a, p, st);
     case PromptKv::kPagedBf16: return launch_kv<PromptKv::kPagedBf16>(a, p, st);
     default:
-      if (p.cols == 256) p.cols = 128, p.tiles = a.T * (a.Hq / a.Hk) / 128 + std::min<int64_t>(a.B, a.T);
+      if (p.cols == 256) p.cols = 128, p.tiles = prompt_tiles(a.T, a.B, a.Hq / a.Hk, 128);
       return launch_kv<PromptKv::kPagedFp8>(a, p, st);
   }
 }

@@ -99,6 +99,30 @@ def test_many_sequences(n):
     check_all(out, None, q, k, v, lens, lens, True)
 
 
+@pytest.mark.parametrize("paged", [False, True], ids=["own", "cache"])
+@pytest.mark.parametrize("n,first", [(65, 0), (129, 5), (4096, 0), (4097, 40), (9000, 1)], ids=str)
+def test_every_sequence_is_found(n, first, paged):
+    """Empty ones, full tiles, more than a tile, and rows before and behind; a sample against 64 bits."""
+    lens = [(0, 1, 3, 0, 64, 1, 0, 2, 33)[(i + i // 9) % 9] if i % 500 != 77 else 300 for i in range(n)]
+    T, g = sum(lens) + first + 9, gen(n)
+    out = torch.full((T, 6, 64), float("nan"), device=DEV).bfloat16()
+    q, k, v = heads(T, (6, 2, 2), 64, g)
+    s = starts(lens, first)
+    if paged:
+        kv, scales, table = cache_of([m + i % 70 for i, m in enumerate(lens)], 2, 64, 16, "bf16", g)
+        klens = torch.tensor([m + i % 70 for i, m in enumerate(lens)], dtype=torch.int32, device=DEV)
+        jb.jq_chunk_attention(q, *kv, table, s, klens, out=out)
+    else:
+        jb.jq_prompt_attention(q, k, v, s, out=out)
+    assert out[:first].isnan().all() and out[T - 9:].isnan().all() and not out[first:T - 9].isnan().any()
+    at = s.tolist()
+    for b in {*range(0, n, max(1, n // 60)), *range(n - 5, n)} | {b for b in range(n) if lens[b] == 300}:
+        i, j = at[b], at[b + 1]
+        if j > i:
+            kb, vb = rows_of(kv, scales, table, b, lens[b] + b % 70) if paged else (k[i:j], v[i:j])
+            ref.check_attention(out[i:j], None, q[i:j], kb, vb, True, None)
+
+
 @pytest.mark.parametrize("klen", [0, 3000], ids=["own", "long"])
 def test_rows_of_no_sequence_stay(klen):
     """Rows before the first and behind the last sequence, with one part and with several."""
