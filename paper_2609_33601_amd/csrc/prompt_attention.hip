@@ -405,24 +405,33 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) dma16(rv, dst + Z::kHalf + 1024 * i, v_off[i], 0);
   };
-  // e4m3: through registers, widened to bf16 (exactly) on the way
-  u32x4 kr[kFp8 ? kLoads : 1], vr[kFp8 ? kLoads : 1];
+  // e4m3: through registers, widened to bf16 (exactly) on the way.  At D = 256,
+  // where registers are short, keys and values have the same ones in turn: keys
+  // are put after a step's scores, values after its sums, each asked for half a
+  // step before (2048 tokens over 16384, 16 heads of 256: 681 us; with both at
+  // once, and 65 registers in memory, 1192; at D = 128 that way 1199 instead of
+  // 1170 for 2048 over 32768, and 154 instead of 145 for a ragged batch).
+  constexpr bool kTurns = kFp8 && D == 256;
+  u32x4 kr[kFp8 ? kLoads : 1], vr[kFp8 && !kTurns ? kLoads : 1];
   float sr = 0.0f;
-  auto fetch = [&](int t0) __attribute__((always_inline)) {
+  Src held{};
+  auto load_rows = [&](u32x4* r, const uint8_t* p) __attribute__((always_inline)) {
     if constexpr (kFp8) {
-      const Src s = source(t0);
-      const int n = span(s, D);
-      const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.k), 0, n, kRawBuffer);
-      const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.v), 0, n, kRawBuffer);
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, span(held, D), kRawBuffer);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off[i], 0, 0));
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, v_off[i], 0, 0));
-      // lanes 0 .. 31 a scale of a key each, 32 .. 63 of a value
-      sr = li < s.rows ? (lh ? a.v_scale : a.k_scale)[s.line + li] : 0.0f;
+      for (int i = 0; i < kLoads; ++i) r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_off[i], 0, 0));
     }
   };
-  auto put = [&](int buf) __attribute__((always_inline)) {
+  auto fetch = [&](int t0) __attribute__((always_inline)) {
+    if constexpr (kFp8) {
+      held = source(t0);
+      load_rows(kr, held.k);
+      if constexpr (!kTurns) load_rows(vr, held.v);
+      // lanes 0 .. 31 a scale of a key each, 32 .. 63 of a value
+      sr = li < held.rows ? (lh ? a.v_scale : a.k_scale)[held.line + li] : 0.0f;
+    }
+  };
+  auto put_rows = [&](int buf, const u32x4* r, bool values) __attribute__((always_inline)) {
     if constexpr (kFp8) {
       uint8_t* base = lds + buf * Z::kStage;
 #pragma unroll
@@ -430,20 +439,38 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         const int rr = wave * kWaveRows + i * (64 / kPerRow) + lane / kPerRow, c = 2 * (lane % kPerRow);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          u32x4 kk, vv;
+          u32x4 w;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            kk[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kr[i][2 * h + j], 1.0f, false));
-            kk[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kr[i][2 * h + j], 1.0f, true));
-            vv[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(vr[i][2 * h + j], 1.0f, false));
-            vv[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(vr[i][2 * h + j], 1.0f, true));
+            w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[i][2 * h + j], 1.0f, false));
+            w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[i][2 * h + j], 1.0f, true));
           }
-          *reinterpret_cast<u32x4*>(base + rr * Z::kRow + 16 * key_slot<D>(rr, c + h)) = kk;
-          *reinterpret_cast<u32x4*>(base + Z::kHalf + rr * Z::kRow + 16 * value_slot<D>(rr, c + h)) = vv;
+          uint8_t* dst = base + rr * Z::kRow + (values ? Z::kHalf + 16 * value_slot<D>(rr, c + h) : 16 * key_slot<D>(rr, c + h));
+          *reinterpret_cast<u32x4*>(dst) = w;
         }
       }
+    }
+  };
+  auto put_keys = [&](int buf) __attribute__((always_inline)) {
+    if constexpr (kFp8) {
+      put_rows(buf, kr, false);
       if (li < kWaveRows)
-        *reinterpret_cast<float*>(base + 2 * Z::kHalf + 4 * (lh * kKeys + wave * kWaveRows + li)) = sr;
+        *reinterpret_cast<float*>(lds + buf * Z::kStage + 2 * Z::kHalf + 4 * (lh * kKeys + wave * kWaveRows + li)) = sr;
+    }
+  };
+  // what is between step i's scores and its sums, and after them, at D = 256
+  auto keys_turn = [&](int i) __attribute__((always_inline)) {
+    if constexpr (kTurns) {
+      if (i + 1 >= steps) return;
+      put_keys((i + 1) & 1);
+      load_rows(kr, held.v);
+    }
+  };
+  auto values_turn = [&](int i) __attribute__((always_inline)) {
+    if constexpr (kTurns) {
+      if (i + 1 >= steps) return;
+      put_rows((i + 1) & 1, kr, true);
+      if (i + 2 < steps) fetch(t_begin + (i + 2) * kKeys);
     }
   };
 
@@ -466,7 +493,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   };
 
   // The keys t0 .. of a stage: all of them, or half `part` of them.
-  auto step = [&](const uint8_t* stage, int t0, int part, auto count, auto mask) __attribute__((always_inline)) {
+  auto step = [&](const uint8_t* stage, int t0, int index, int part, auto count, auto mask) __attribute__((always_inline)) {
     constexpr int kSub = decltype(count)::value;
     constexpr bool kMask = decltype(mask)::value;
     const uint8_t* base = stage + part * 32 * Z::kRow;
@@ -486,6 +513,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         for (int g = 0; g < QG; ++g) s[n][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[g][c], s[n][g], 0, 0, 0);
       }
     }
+    keys_turn(index);
     if constexpr (kFp8) {
 #pragma unroll
       for (int n = 0; n < kSub; ++n)
@@ -526,9 +554,10 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
         m[g] = more ? top : m[g];
         l[g] *= keep;
 #pragma unroll
-        for (int t = 0; t < kOut; ++t)
+        for (int t = 0; t < kOut; ++t) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[t][g][i] *= keep;
+        }
       }
       const float base_m = m[g] == kNegInf ? 0.0f : m[g];
 #pragma unroll
@@ -572,12 +601,15 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
 #pragma unroll
         for (int g = 0; g < QG; ++g) o[t][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k16][g], o[t][g], 0, 0, 0);
       }
+    values_turn(index);
   };
 
   if (steps > 0) {
     if constexpr (kFp8) {
       fetch(t_begin);
-      put(0);
+      put_keys(0);
+      if constexpr (kTurns) load_rows(kr, held.v);
+      put_rows(0, kTurns ? kr : vr, true);
       if (steps > 1) fetch(t_begin + kKeys);
     } else {
       issue(0, t_begin);
@@ -587,8 +619,9 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   auto arrive = [&](int i) __attribute__((always_inline)) {
     if constexpr (kFp8) {
       __syncthreads();
-      if (i + 1 >= steps) return;
-      put((i + 1) & 1);
+      if (kTurns || i + 1 >= steps) return;
+      put_keys((i + 1) & 1);
+      put_rows((i + 1) & 1, vr, true);
       if (i + 2 < steps) fetch(t_begin + (i + 2) * kKeys);
     } else if (i == 0 && steps > 1) {
       // both buffers' transfers are on their way
@@ -609,21 +642,25 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
     if constexpr (Z::kUnroll) {
       for (; i + 1 < plain; i += 2) {
         arrive(i);
-        step(lds, t_begin + i * kKeys, part, count, std::false_type());
+        step(lds, t_begin + i * kKeys, i, part, count, std::false_type());
         arrive(i + 1);
-        step(lds + Z::kStage, t_begin + (i + 1) * kKeys, part, count, std::false_type());
+        step(lds + Z::kStage, t_begin + (i + 1) * kKeys, i + 1, part, count, std::false_type());
       }
     } else {
       for (; i < plain; ++i) {
         arrive(i);
-        step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, part, count, std::false_type());
+        step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, i, part, count, std::false_type());
       }
     }
     for (; i < seen; ++i) {
       arrive(i);
-      step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, part, count, std::true_type());
+      step(lds + (i & 1) * Z::kStage, t_begin + i * kKeys, i, part, count, std::true_type());
     }
-    for (; i < steps; ++i) arrive(i);
+    for (; i < steps; ++i) {
+      arrive(i);
+      keys_turn(i);
+      values_turn(i);
+    }
   };
   if (halves) run(wave >> 1, std::integral_constant<int, 1>());
   else run(0, std::integral_constant<int, 2>());
