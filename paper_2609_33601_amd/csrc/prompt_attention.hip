@@ -864,8 +864,9 @@ hipError_t launch_kv(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
 // shapes (1 to 64 sequences, 1 to 1024 new tokens, 600 to 32768 cached, equal
 // and ragged, both caches, every choice of columns and parts timed): a step of
 // 64 keys, alone on a CU or in pairs, for 128 columns and for up to 64, and the
-// join.  The choice by this is 3.4% from the best one on average; a fixed
-// number of blocks a CU was 21%.
+// join.  On 258 shapes, 218 of them drawn at random, the choice by this is 3.8%
+// from the best one on average and 39% at most; a fixed number of blocks a CU
+// was 21% on average.
 static float prompt_cost(int64_t cols, int64_t blocks, int64_t steps, int64_t parts, int64_t rows, int64_t D, bool half) {
   constexpr float kAlone[2] = {1.15f, 0.85f}, kPair[2] = {1.84f, 1.11f}, kWhole = 0.6f;
   const float n = static_cast<float>(blocks);
@@ -888,7 +889,11 @@ static int64_t prompt_tiles(int64_t T, int64_t B, int64_t G, int64_t cols) {
 
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
   const int64_t G = Hq / Hk, expect = paged ? max_len : (max_len + B - 1) / B;  // keys of a sequence
-  auto blocks_of = [&](int64_t cols) { return std::max((T * G + cols - 1) / cols, std::min(B, T)) * Hk; };
+  // a tile a sequence, or, of longer ones, the last tile half full
+  auto blocks_of = [&](int64_t cols) {
+    const int64_t n = std::min(B, T);
+    return (T * G <= cols * n ? n : (T * G + cols - 1) / cols + n / 2) * Hk;
+  };
   PromptPlan p;
   p.parts = 1;
   p.chunk = (max_len + 63) / 64 * 64;
@@ -907,7 +912,7 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
       for (int64_t parts = 1; parts <= 256; parts += (parts + 3) / 4) {
         // Parts of the longest that a sequence may be; one as long as expected has
         // `used` of them (8 sequences of 16 on 4096 keys: 59 us uncut, 39 so; 4 of
-        // 77 on 4608, 24 heads: 67 and 56).
+        // 16 on 8192, 16 heads of 256 on 4: 72 and 53).
         const int64_t chunk = ((max_len + parts - 1) / parts + 63) / 64;  // steps
         const int64_t used = (expect + 64 * chunk - 1) / (64 * chunk);
         if (parts > 1 && (!cut || chunk < 2 || blocks * parts >= 1 << 20)) break;
