@@ -110,10 +110,11 @@ struct PromptArgs {
   PromptKv kv;
 };
 // How a call is cut: columns (new tokens times heads that share a key head) of
-// a tile, the most tiles that the sequences can have, keys of a part, parts.
+// a tile, the most parts of a sequence's keys and the fewest keys of one, the
+// most tiles that the sequences can have.
 struct PromptPlan {
-  int cols, parts;
-  int64_t tiles, chunk;
+  int cols, parts, least;
+  int64_t tiles;
 };
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged);
 hipError_t launch_prompt_attention(const PromptArgs& a, PromptPlan p, hipStream_t st);

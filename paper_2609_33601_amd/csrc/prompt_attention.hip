@@ -286,7 +286,7 @@ __device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int tok
 
 template <int D, int QG, PromptKv KV>
 __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt_attention_kernel(
-    const PromptArgs a, int tiles, int per, int chunk, int parts) {
+    const PromptArgs a, int tiles, int per, int parts, int least) {
   using Z = Sizes<D, QG, KV>;
   constexpr bool kFp8 = KV == PromptKv::kPagedFp8, kPaged = KV != PromptKv::kDense;
   constexpr int kKeys = Z::kKeys, kSteps = D / 16, kOut = D / 32, kWaveRows = kKeys / 4;
@@ -315,6 +315,9 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   auto limit = [&](int col) { return a.causal ? min(max(nk - at.rows + col / G + 1, 0), nk) : nk; };
   const int block_end = limit(last_col);
   const int wave_end = limit(min(wcol + 32 * QG, cols) - 1), wave_all = limit(min(wcol, cols - 1));
+  // Its part of the keys: every sequence is cut by its own length, so the bound
+  // that the host knows decides only how many parts there may be.
+  const int chunk = parts == 1 ? nk : max(((nk - 1) / parts / 64 + 1) * 64, least);
   const int t_begin = min(static_cast<int64_t>(part) * chunk, static_cast<int64_t>(block_end));
   const int t_end = min(block_end - t_begin, chunk) + t_begin;
   const int steps = (t_end - t_begin + kKeys - 1) / kKeys;
@@ -840,7 +843,7 @@ template <int D, int QG, PromptKv KV>
 void launch_tiles(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>(p.tiles * a.Hk * p.parts));
   hipLaunchKernelGGL((prompt_attention_kernel<D, QG, KV>), grid, dim3(kThreads), 0, st, a, static_cast<int>(p.tiles),
-                     p.cols, static_cast<int>(p.chunk), p.parts);
+                     p.cols, p.parts, p.least);
 }
 
 template <int D, PromptKv KV>
@@ -872,9 +875,9 @@ hipError_t launch_kv(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
 // shapes (1 to 64 sequences, 1 to 1024 new tokens, 600 to 32768 cached, equal
 // and ragged, both caches, every choice of columns and parts timed): a step of
 // 64 keys, alone on a CU or in pairs, for 128 columns and for up to 64, and the
-// join.  On 258 shapes, 218 of them drawn at random, the choice by this is 3.8%
-// from the best one on average and 39% at most; a fixed number of blocks a CU
-// was 21% on average.
+// join.  On 220 shapes drawn at random the choice by this is 2.9% from the best
+// one on average and 39% at most; a fixed number of blocks a CU was 21% on
+// average of the 71.
 static float prompt_cost(int64_t cols, int64_t blocks, int64_t steps, int64_t parts, int64_t rows, int64_t D, bool half) {
   constexpr float kAlone[2] = {1.15f, 0.85f}, kPair[2] = {1.84f, 1.11f}, kWhole = 0.6f;
   const float n = static_cast<float>(blocks);
@@ -903,8 +906,7 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
     return (T * G <= cols * n ? n : (T * G + cols - 1) / cols + n / 2) * Hk;
   };
   PromptPlan p;
-  p.parts = 1;
-  p.chunk = (max_len + 63) / 64 * 64;
+  p.parts = 1, p.least = 0;
   if (D == 64 && T * G / 256 * Hk >= 512) {
     // columns enough for blocks of 256, whose waves read a key for 64 columns
     // instead of 32 (4096 tokens, 32 heads: 167 us with 128, 146 with 256)
@@ -918,24 +920,21 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
       const int64_t blocks = blocks_of(cols);
       const bool half = cols == 64 || T * G <= 64 * std::min(B, T);
       for (int64_t parts = 1; parts <= 256; parts += (parts + 3) / 4) {
-        // Parts of the longest that a sequence may be; one as long as expected has
-        // `used` of them (8 sequences of 16 on 4096 keys: 59 us uncut, 39 so; 4 of
-        // 16 on 8192, 16 heads of 256 on 4: 72 and 53).
-        const int64_t chunk = ((max_len + parts - 1) / parts + 63) / 64;  // steps
-        const int64_t used = (expect + 64 * chunk - 1) / (64 * chunk);
+        const int64_t chunk = ((expect + parts - 1) / parts + 63) / 64;  // steps
         if (parts > 1 && (!cut || chunk < 2 || blocks * parts >= 1 << 20)) break;
-        if (parts > 1 && used == 1) continue;
-        const int64_t all = (max_len + 64 * chunk - 1) / (64 * chunk);
-        float us = prompt_cost(cols, blocks * used, std::min(chunk, (expect + 63) / 64), all, T * Hq, D, half);
-        us += 3.0f / 512.0f * static_cast<float>(blocks * (all - used));  // blocks that find nothing to do
+        const int64_t used = (expect + 64 * chunk - 1) / (64 * chunk);
+        const float us = prompt_cost(cols, blocks * used, chunk, used, T * Hq, D, half);
         if (best == 0.0f || us < best) {
           best = us;
           p.cols = cols;
-          p.chunk = 64 * chunk;
+          p.parts = static_cast<int>(used);
+          // A shorter sequence has as many parts, but none below this: with 128 keys
+          // at least, a ragged batch of chunks and single tokens takes 153 us
+          // instead of 145, 8 x 64 tokens over 2000 under a limit of 131072 77 and 54.
+          p.least = static_cast<int>(std::min<int64_t>(64 * chunk, 512));
         }
       }
     }
-    p.parts = static_cast<int>((max_len + p.chunk - 1) / p.chunk);
   }
   p.tiles = prompt_tiles(T, B, G, p.cols);
   return p;

@@ -224,8 +224,8 @@ def jq_chunk_attention(q, k_cache, v_cache, page_table, starts, lens, k_scale=No
     tokens, the new ones among them; returns bf16 [T,Hq,D].
 
     Sequence b has the rows starts[b] .. starts[b+1] (int32 [B+1]) of q, lens[b] (int32 [B]) cached tokens and the pages
-    page_table[b] (int32 [B,columns]).  max_len bounds the lengths (the table's capacity by default) and decides how the
-    cache is split; the rest is as at jq_prompt_attention.
+    page_table[b] (int32 [B,columns]).  max_len bounds the lengths (the table's capacity by default) and decides into how
+    many parts a sequence's keys may be split; the rest is as at jq_prompt_attention.
     """
     return _done(_native.chunk_attention(q, k_cache, v_cache, page_table, starts, lens, k_scale, v_scale, max_len,
                                          sm_scale, causal, out, lse, workspace, _stream(stream)), "jq_chunk_attention")

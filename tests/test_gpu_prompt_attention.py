@@ -289,6 +289,22 @@ def test_chunk_many_columns(D, Hq, Hk, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("limit", [2100, 9000, 1 << 20])
+def test_chunk_under_a_long_limit(limit, D, kind):
+    """Each sequence is cut by its own length: ends of parts, and a last part of one key."""
+    new, lens, g = [40, 1, 3, 64, 1, 20], [513, 1025, 5, 2049, 0, 1537], gen(limit + D)
+    kv, scales, table = cache_of(lens, 2, D, 16, kind, g)
+    wide = torch.full((6, -(-limit // 16)), 1 << 30, dtype=torch.int32, device=DEV)
+    wide[:, : table.shape[1]] = table[:, : wide.shape[1]]
+    q = torch.randn((sum(new), 8, D), generator=g, device=DEV).bfloat16()
+    lse = torch.empty((sum(new), 8), device=DEV)
+    out = jb.jq_chunk_attention(q, *kv, wide, starts(new), torch.tensor(lens, dtype=torch.int32, device=DEV), *scales,
+                                max_len=limit, lse=lse)
+    check_chunk(out, lse, q, kv, scales, table, new, lens, True)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
 def test_chunk_max_len_bounds_lengths(kind):
     g = gen(11)
     kv, scales, table = cache_of([500, 40], 2, 128, 16, kind, g)
