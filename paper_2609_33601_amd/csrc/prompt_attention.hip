@@ -110,12 +110,13 @@ __device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, 
   int first = 0;  // of 64 sequences, a lane each
   int slot = tiles - 1 - index;
   if (many) {
-    // Sequence b has the places from starts[b] G / per + b on, as many as it needs
-    // or one more, so a search finds it (4096 sequences of one token over up to
-    // 64, 8 key heads: 350 us, by a walk along all sequences 960).
+    // Sequence b has the places from starts[b] G / per + min(b, starts[b]) on, as
+    // many as it needs or more, so a search finds it (4096 sequences of one token
+    // over up to 64, 8 key heads: 350 us, by a walk along all sequences 960).
     for (int step = a.B > 4096 ? 4096 : 64; step > 1; step /= 64) {
       const int b = first + lane * step;
-      const int from = b < a.B ? (min(max(a.starts[b], 0), static_cast<int>(a.T)) * G >> shift) + b : slot + 1;
+      const int start = b < a.B ? min(max(a.starts[b], 0), static_cast<int>(a.T)) : 0;
+      const int from = b < a.B ? (start * G >> shift) + min(b, start) : slot + 1;
       const uint64_t hit = __ballot(from <= slot);
       if (hit == 0) break;  // and below
       first += (63 - __builtin_clzll(hit)) * step;
@@ -132,7 +133,7 @@ __device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, 
   const int n = (rows * G + per - 1) >> shift;
   int tile, l;
   if (many) {
-    tile = slot - ((row0 * G >> shift) + b);
+    tile = slot - ((row0 * G >> shift) + min(b, row0));
     const uint64_t hit = __ballot(b < a.B && tile >= 0);
     l = hit == 0 ? 0 : 63 - __builtin_clzll(hit);
   } else {
@@ -892,11 +893,8 @@ static float prompt_cost(int64_t cols, int64_t blocks, int64_t steps, int64_t pa
   return us;
 }
 
-// Places for tiles: the most tiles that B sequences of T tokens have; where they
-// are searched (find_tile), one for each sequence besides the full ones.
-static int64_t prompt_tiles(int64_t T, int64_t B, int64_t G, int64_t cols) {
-  return T * G / cols + (B > 64 ? B : std::min(B, T));
-}
+// The most tiles that B sequences of T tokens have.
+static int64_t prompt_tiles(int64_t T, int64_t B, int64_t G, int64_t cols) { return T * G / cols + std::min(B, T); }
 
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged) {
   const int64_t G = Hq / Hk, expect = paged ? max_len : (max_len + B - 1) / B;  // keys of a sequence

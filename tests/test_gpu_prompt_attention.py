@@ -123,6 +123,22 @@ def test_every_sequence_is_found(n, first, paged):
             ref.check_attention(out[i:j], None, q[i:j], kb, vb, True, None)
 
 
+@pytest.mark.parametrize("at", ["first", "last", "apart"])
+@pytest.mark.parametrize("n", [100, 5000, 65536])
+def test_few_tokens_of_many_sequences(n, at):
+    """A padded batch: most sequences are empty, there are more of them than tokens."""
+    g, some = gen(n), [5, 1, 40, 2, 1]
+    where = {"first": range(5), "last": range(n - 5, n), "apart": [0, 7, n // 2, n // 2 + 1, n - 2]}[at]
+    lens = [0] * n
+    for b, m in zip(where, some):
+        lens[b] = m
+    q, k, v = heads(50, (6, 2, 2), 64, g)
+    out = torch.full((50, 6, 64), float("nan"), device=DEV).bfloat16()
+    jb.jq_prompt_attention(q, k, v, starts(lens), out=out)
+    check_all(out[:49], None, q, k, v, some, some, True)
+    assert out[49:].isnan().all()
+
+
 @pytest.mark.parametrize("klen", [0, 3000], ids=["own", "long"])
 def test_rows_of_no_sequence_stay(klen):
     """Rows before the first and behind the last sequence, with one part and with several."""
