@@ -37,7 +37,7 @@
 // the vector instructions taken out gave 1 to 2%.  A large library product runs
 // at 1450 TFLOP/s on this card.  4608 tokens, 24 heads of 128, all of them seen:
 // 272 us, 960 TFLOP/s (864 equal blocks for 512 places); 8192 causal, 32 on 8
-// heads: 511, 1076; 2048 over 32768 cached: 971, 1097, and from e4m3 1164, whose
+// heads: 508, 1082; 2048 over 32768 cached: 965, 1105, and from e4m3 1155, whose
 // scales and widening are 130 more instructions a step.  Three prompts of up to
 // 77 tokens: 5.9 us, a launch and three steps' chain; 16 tokens over 2080: 12.4,
 // two launches.
@@ -317,10 +317,12 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   const int block_end = limit(last_col);
   const int wave_end = limit(min(wcol + 32 * QG, cols) - 1), wave_all = limit(min(wcol, cols - 1));
   // Its part of the keys: every sequence is cut by its own length, so the bound
-  // that the host knows decides only how many parts there may be.
+  // that the host knows decides only how many parts there may be.  The bounds go
+  // to scalar registers by hand: left to itself the compiler works out a step's
+  // rows in vector ones (2048 tokens over 32768: 983 us instead of 965).
   const int chunk = parts == 1 ? nk : max(((nk - 1) / parts / 64 + 1) * 64, least);
-  const int t_begin = min(static_cast<int64_t>(part) * chunk, static_cast<int64_t>(block_end));
-  const int t_end = min(block_end - t_begin, chunk) + t_begin;
+  const int t_begin = __builtin_amdgcn_readfirstlane(min(static_cast<int64_t>(part) * chunk, static_cast<int64_t>(block_end)));
+  const int t_end = __builtin_amdgcn_readfirstlane(min(block_end - t_begin, chunk) + t_begin);
   const int steps = (t_end - t_begin + kKeys - 1) / kKeys;
 
   // queries
