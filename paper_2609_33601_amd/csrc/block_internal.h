@@ -117,11 +117,17 @@ struct PromptPlan {
   int64_t tiles;
 };
 PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged);
+// The same for what holds the keys (8-bit caches have no tiles of 256 columns).
+PromptPlan prompt_plan_of(PromptPlan p, int64_t T, int64_t B, int64_t G, PromptKv kv);
 hipError_t launch_prompt_attention(const PromptArgs& a, PromptPlan p, hipStream_t st);
 
 }  // namespace jq
 
 // For the tests only (no part of the C ABI): the kernel that a product takes.
 extern "C" int jq_internal_fp8_route(int64_t M, int64_t N, int64_t K, int64_t cus);
+// The same for a call of jq_prompt_attention (kv 0, max_len its Tk) or
+// jq_chunk_attention (1 bf16, 2 8-bit): out = columns of a tile, parts; a jq_status.
+extern "C" int jq_internal_prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, int kv,
+                                       int out[2]);
 
 #endif  // JQ_BLOCK_INTERNAL_H

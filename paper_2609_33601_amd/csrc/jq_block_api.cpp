@@ -370,6 +370,15 @@ jq_status jq_gated_act(const void* gate, int64_t gate_stride, const void* up, in
   return from_hip(jq::launch_gated_act(a, static_cast<jq::Act>(act), static_cast<jq::NormOut>(out), as_stream(stream)));
 }
 
+int jq_internal_prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, int kv, int out[2]) {
+  jq::PromptPlan p;
+  const jq_status st = plan_prompt(T, B, Hq, Hk, D, max_len, kv != 0, &p);
+  if (st != JQ_OK) return st;
+  p = jq::prompt_plan_of(p, T, B, Hq / Hk, static_cast<jq::PromptKv>(kv));
+  out[0] = p.cols, out[1] = p.parts;
+  return JQ_OK;
+}
+
 size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int64_t Hq, int64_t Hk, int64_t D) {
   return prompt_workspace_bytes(T, B, Hq, Hk, D, Tk, false);
 }

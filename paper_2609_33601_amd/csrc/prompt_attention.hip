@@ -940,13 +940,17 @@ PromptPlan prompt_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, 
   return p;
 }
 
+PromptPlan prompt_plan_of(PromptPlan p, int64_t T, int64_t B, int64_t G, PromptKv kv) {
+  if (kv == PromptKv::kPagedFp8 && p.cols == 256) p.cols = 128, p.tiles = prompt_tiles(T, B, G, 128);
+  return p;
+}
+
 hipError_t launch_prompt_attention(const PromptArgs& a, PromptPlan p, hipStream_t st) {
+  p = prompt_plan_of(p, a.T, a.B, a.Hq / a.Hk, a.kv);
   switch (a.kv) {
     case PromptKv::kDense: return launch_kv<PromptKv::kDense>(a, p, st);
     case PromptKv::kPagedBf16: return launch_kv<PromptKv::kPagedBf16>(a, p, st);
-    default:
-      if (p.cols == 256) p.cols = 128, p.tiles = prompt_tiles(a.T, a.B, a.Hq / a.Hk, 128);
-      return launch_kv<PromptKv::kPagedFp8>(a, p, st);
+    default: return launch_kv<PromptKv::kPagedFp8>(a, p, st);
   }
 }
 
