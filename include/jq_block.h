@@ -261,8 +261,9 @@ size_t jq_prompt_attention_workspace_bytes(int64_t T, int64_t Tk, int64_t B, int
  * end before it begins as empty; where they decrease, what the rows hold is
  * unspecified, and nothing outside the arrays is touched.
  * An infinity or NaN among a token's values reaches the queries that see the
- * token, and no other; a score of -infinity is a weight of 0.  The weights are
- * rounded to bf16 for the product with the values; scores, statistics and sums are fp32.
+ * token, and no other (the call then takes up to eight times as long); a score
+ * of -infinity is a weight of 0.  The weights are rounded to bf16 for the product
+ * with the values; scores, statistics and sums are fp32.
  * D = 64, 128 or 256; Hq % Hk == 0; T, Tk <= 2^30, B <= 65536, T * Hq < 2^31 and
  * T * Hq / 128 + 2 * min(B, T) * Hk < 2^24;
  * strides % 8 == 0, at least a token's elements, k_stride and v_stride <= 2^25.

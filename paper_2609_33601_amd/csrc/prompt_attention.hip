@@ -201,88 +201,177 @@ __device__ __forceinline__ int64_t row_place(const PromptArgs& a, int seq, int h
     return *line * D;
   }
 }
+// Elements i .. i + 7 of a row, and one of them, as bf16.
 template <PromptKv KV>
-__device__ __forceinline__ float one_value(const void* p, int64_t i) {
+__device__ __forceinline__ u32x4 eight_of(const void* p, int64_t i) {
+  if constexpr (KV == PromptKv::kPagedFp8) {
+    const u32x2 u = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(p) + i);
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[j], 1.0f, false));
+      w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[j], 1.0f, true));
+    }
+    return w;
+  } else {
+    return *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + i);
+  }
+}
+template <PromptKv KV>
+__device__ __forceinline__ uint32_t one_of(const void* p, int64_t i) {
   if constexpr (KV == PromptKv::kPagedFp8) {
     const uint32_t u = static_cast<const uint8_t*>(p)[i];
-    return bf_lo(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, false)) & 0xFFFFu);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, false)) & 0xFFFFu;
   } else {
-    return bf_lo(static_cast<const uint16_t*>(p)[i]);
+    return static_cast<const uint16_t*>(p)[i];
   }
 }
+__device__ __forceinline__ bool odd_bf16(uint32_t u) { return (u & 0x7F80u) == 0x7F80u; }
 
-// Whether any value of the tokens [t0, t1) is an infinity or NaN; for one wave.
-template <int D, PromptKv KV>
-__device__ __forceinline__ bool odd_values(const PromptArgs& a, int seq, int hk, int key0, int t0, int t1) {
-  float sum = 0.0f;
-  for (int t = t0 + (threadIdx.x & 63); t < t1; t += 64) {
-    int64_t line;
-    const int64_t at = row_place<D, KV>(a, seq, hk, key0, t, a.v_stride, &line);
-    for (int d = 0; d < D; ++d) sum = fmaf(one_value<KV>(a.v, at + d), 0.0f, sum);
-  }
-  return __any(sum != 0.0f) != 0;
-}
-
-// One column's keys [t0, t1) by one wave, in fp32 and straight from memory: for
-// columns beside which a product met an infinity or NaN among the values of
-// tokens that only some of its columns see (such a value times a weight of 0
-// would count).  A lane takes a key at a time for the scores and D / 64 values
-// of the output.  Nothing of the fast path is alive here, so it costs that path
-// no registers (masks inside its product took 70 more).
-template <int D, PromptKv KV>
-__device__ __forceinline__ void one_column(const PromptArgs& a, int seq, int token, int head, int hk, int key0, int t0, int t1,
-                                        int part, int parts, bool bad) {
-  constexpr int kPer = D / 64;
+// Calls f(t) for the tokens [t0, t1) that have an infinity or NaN among their
+// values, until it returns false; for one wave, eight values a lane.
+template <int D, PromptKv KV, class F>
+__device__ __forceinline__ void for_odd_values(const PromptArgs& a, int seq, int hk, int key0, int t0, int t1, F f) {
+  constexpr int kPieces = D / 8, kRows = 64 / kPieces;
   const int lane = threadIdx.x & 63;
-  const uint16_t* q = a.q + static_cast<int64_t>(token) * a.q_stride + static_cast<int64_t>(head) * D;
+  for (int t = t0; t < t1; t += kRows) {
+    bool odd = false;
+    if (t + lane / kPieces < t1) {
+      int64_t line;
+      const int64_t at = row_place<D, KV>(a, seq, hk, key0, t + lane / kPieces, a.v_stride, &line);
+      const u32x4 w = eight_of<KV>(a.v, at + 8 * (lane % kPieces));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) odd |= odd_bf16(w[j]) || odd_bf16(w[j] >> 16);
+    }
+    const uint64_t hit = __ballot(odd);
+#pragma unroll 1
+    for (int r = 0; r < kRows; ++r)
+      if ((hit >> (r * kPieces) & ((1ull << kPieces) - 1)) != 0 && !f(t + r)) return;
+  }
+}
+
+// A wave's 32 columns over the keys [t0, t1), straight from memory: for columns
+// beside which a product met an infinity or NaN among the values of tokens that
+// only some of them see, which such a value's weight of 0 does not take away.
+// Values of the tokens from `all` on, which some columns do not see, are read as
+// 0 where they are not finite, and those tokens are put in afterwards, for the
+// columns that see them.  Nothing of the fast path is alive here, so it costs
+// that path no registers (masks inside its product took 70 more).
+//
+// Bound by the latency of its loads, 4 us for 32 keys: 2048 tokens over 32768
+// with all new tokens' values NaN take 6.3 ms instead of 1.0, 512 over 2048 91
+// us instead of 24 (one column after the other, a key a lane: 3700).
+template <int D, PromptKv KV>
+__device__ __forceinline__ void wave_columns(const PromptArgs& a, int seq, int hk, int key0, int t0, int t1, int all,
+                                             const uint16_t* q_row, int lim, f32x16* o, float* m, float* l) {
+  constexpr bool kFp8 = KV == PromptKv::kPagedFp8;
+  constexpr int kSteps = D / 16, kOut = D / 32;
+  const int li = threadIdx.x & 31, lh = threadIdx.x >> 5 & 1;
   auto place = [&](int t, int64_t stride, int64_t* line) { return row_place<D, KV>(a, seq, hk, key0, t, stride, line); };
-  const float scale2 = power_scale(a.scale), sign = a.scale < 0.0f ? -1.0f : 1.0f;
-  float m = kNegInf, l = 0.0f, acc[kPer];
+  const float scale2 = power_scale(a.scale);
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+  lim = min(lim, t1);
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) acc[j] = 0.0f;
-  for (int t = t0; t < t1; t += 64) {
-    float s = kNegInf;
+  for (int n = 0; n < kOut; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[n][i] = 0.0f;
+  float top = kNegInf, sum = 0.0f;
+#pragma unroll 1
+  for (int t = t0; t < t1; t += 32) {
     int64_t line = 0;
-    if (t + lane < t1) {
-      const int64_t at = place(t + lane, a.k_stride, &line);
-      float dot = 0.0f;
-      for (int d = 0; d < D; ++d) dot = fmaf(bf_lo(q[d]), one_value<KV>(a.k, at + d), dot);
-      if constexpr (KV == PromptKv::kPagedFp8) dot *= a.k_scale[line];
-      s = sign * dot * scale2;
+    const int64_t k_row = place(min(t + li, t1 - 1), a.k_stride, &line);
+    float k_scale = 1.0f, v_scale = 1.0f;  // of key li
+    if constexpr (kFp8) k_scale = a.k_scale[line], v_scale = a.v_scale[line];
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(q_row + 16 * c) ^ flip;
+      const bf16x8 k = __builtin_bit_cast(bf16x8, eight_of<KV>(a.k, k_row + 16 * c + 8 * lh));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, x), s, 0, 0, 0);
     }
-    float top = s;
+    float next = top;
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-    const float next = fmaxf(m, top), base = next == kNegInf ? 0.0f : next;
-    const float keep = __builtin_amdgcn_exp2f(m - base), p = __builtin_amdgcn_exp2f(s - base);
-    float sum = p;
+    for (int i = 0; i < 16; ++i) {
+      const int j = 8 * (i / 4) + 4 * lh + i % 4;
+      if constexpr (kFp8) s[i] *= __shfl(k_scale, j, 64);
+      s[i] = t + j < lim ? s[i] * scale2 : kNegInf;
+      next = fmaxf(next, s[i]);
+    }
+    next = max_halves(next);
+    const float base = next == kNegInf ? 0.0f : next, keep = __builtin_amdgcn_exp2f(top - base);
+    top = next;
+    sum *= keep;
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, 64);
-    m = next;
-    l = l * keep + sum;
+    for (int n = 0; n < kOut; ++n)
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) acc[j] *= keep;
-    for (int i = 0; i < min(64, t1 - t); ++i) {
-      const int64_t at = place(t + i, a.v_stride, &line);
-      float w = __shfl(p, i, 64);
-      if constexpr (KV == PromptKv::kPagedFp8) w *= a.v_scale[line];
+      for (int i = 0; i < 16; ++i) o[n][i] *= keep;
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) acc[j] = fmaf(w, one_value<KV>(a.v, at + lane * kPer + j), acc[j]);
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+      sum += s[i];
+      if constexpr (kFp8) {
+        const int j = 8 * (i / 4) + 4 * lh + i % 4;
+        const float f = __shfl(v_scale, j, 64);
+        s[i] = t + j < lim ? s[i] * f : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int k16 = 0; k16 < 2; ++k16) {
+      // sixteen keys from a multiple of sixteen on lie in one page
+      const int first = min(t + 16 * k16, t1 - 1), stride = KV == PromptKv::kDense ? static_cast<int>(a.v_stride) : D;
+      const int64_t at = place(first, a.v_stride, &line) + li;
+      float e[8];
+      int off[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        e[j] = s[8 * k16 + j];
+        off[j] = min(8 * (j / 4) + 4 * lh + j % 4, t1 - 1 - first) * stride;
+      }
+      const bf16x8 p = __builtin_bit_cast(bf16x8, pack8_bf16(e));
+#pragma unroll
+      for (int n = 0; n < kOut; ++n) {
+        __builtin_amdgcn_sched_barrier(0);  // eight loads at a time: registers are short
+        uint32_t x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[j] = one_of<KV>(a.v, at + off[j] + 32 * n);
+          if (odd_bf16(x[j]) && t + 16 * k16 + 8 * (j / 4) + 4 * lh + j % 4 >= all) x[j] = 0;
+        }
+        const u32x4 v = {x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p, o[n], 0, 0, 0);
+      }
     }
   }
-  if (bad) l = __builtin_nanf("");
-  const int64_t row = static_cast<int64_t>(token) * a.Hq + head;
-  if (parts > 1) {
-    const int64_t all = a.T * a.Hq, r = part * all + row;
-    if (lane == 0) *reinterpret_cast<float2*>(a.ws + parts * all * D + 2 * r) = float2{m, l};
+  *m = top, *l = sum_halves(sum);
+  for_odd_values<D, KV>(a, seq, hk, key0, max(all, t0), t1, [&](int t) {
+    int64_t line = 0;
+    const int64_t k_row = place(t, a.k_stride, &line) + 8 * lh, v_row = place(t, a.v_stride, &line) + 4 * lh;
+    float dot = 0.0f;
+#pragma unroll 1
+    for (int c = 0; c < kSteps; ++c) {
+      float x[8], k[8];
+      unpack8_bf16(*reinterpret_cast<const u32x4*>(q_row + 16 * c) ^ flip, x);
+      unpack8_bf16(eight_of<KV>(a.k, k_row + 16 * c), k);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) a.ws[r * D + lane * kPer + j] = acc[j];
-  } else {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (a.lse != nullptr && lane == 0) a.lse[row] = log_sum(m, l);
+      for (int j = 0; j < 8; ++j) dot = fmaf(x[j], k[j], dot);
+    }
+    dot = sum_halves(dot);
+    if constexpr (kFp8) dot *= a.k_scale[line];
+    float w = __builtin_amdgcn_exp2f(dot * scale2 - (top == kNegInf ? 0.0f : top));
+    if constexpr (kFp8) w *= a.v_scale[line];
+    if (t < lim) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) a.out[row * D + lane * kPer + j] = static_cast<uint16_t>(pack_bf16(acc[j] * inv, 0.0f));
-  }
+      for (int n = 0; n < kOut; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t v = one_of<KV>(a.v, v_row + 32 * n + 8 * (i / 4) + i % 4);
+          if (odd_bf16(v)) o[n][i] = fmaf(w, bf_lo(v), o[n][i]);
+        }
+    }
+    return true;
+  });
 }
 
 template <int D, int QG, PromptKv KV>
@@ -326,14 +415,13 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   const int steps = (t_end - t_begin + kKeys - 1) / kKeys;
 
   // queries
-  int64_t row[QG];
-  int lim[QG];
+  int row[QG], lim[QG];
   bf16x8 q[QG][kSteps];
 #pragma unroll
   for (int g = 0; g < QG; ++g) {
     const int col = min(wcol + 32 * g + li, cols - 1), token = col / G, head = hk * G + col - token * G;
     lim[g] = limit(col);
-    row[g] = static_cast<int64_t>(at.row0 + token) * a.Hq + head;
+    row[g] = (at.row0 + token) * a.Hq + head;
     const uint16_t* src = a.q + static_cast<int64_t>(at.row0 + token) * a.q_stride + static_cast<int64_t>(head) * D + 8 * lh;
 #pragma unroll
     for (int c = 0; c < kSteps; ++c) {
@@ -722,15 +810,22 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
       for (int t = 0; t < kOut; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum = fmaf(o[t][g][i], 0.0f, sum);
-    if (__any(sum != 0.0f)) leaked = odd_values<D, KV>(a, at.seq, hk, key0, max(wave_all, t_begin), t_end);
+    if (__builtin_expect(__any(sum != 0.0f), 0))
+      for_odd_values<D, KV>(a, at.seq, hk, key0, max(wave_all, t_begin), t_end, [&](int) {
+        leaked = true;
+        return false;
+      });
   }
-  if (leaked) {
-    for (int i = 0; i < 32 * QG && wcol + i < cols; ++i) {
-      const int col = wcol + i, token = col / G;
-      one_column<D, KV>(a, at.seq, at.row0 + token, hk * G + col - token * G, hk, key0, t_begin, min(t_end, limit(col)),
-                        part, parts, bad);
+  if (__builtin_expect(leaked, 0)) {
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      const int col = min(wcol + 32 * g + li, cols - 1), token = col / G, head = hk * G + col - token * G;
+      const uint16_t* src = a.q + static_cast<int64_t>(at.row0 + token) * a.q_stride + static_cast<int64_t>(head) * D + 8 * lh;
+      f32x16 acc[kOut];
+      wave_columns<D, KV>(a, at.seq, hk, key0, t_begin, min(t_end, wave_end), wave_all, src, lim[g], acc, &m[g], &l[g]);
+#pragma unroll
+      for (int t = 0; t < kOut; ++t) o[t][g] = acc[t];
     }
-    return;
   }
 
   // results: lane (li, lh) has values 32 t + 8 (i / 4) + 4 lh + i % 4 of its columns
@@ -755,7 +850,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
       for (int t = 0; t < kOut; ++t)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<u32x2*>(a.out + row[g] * D + 32 * t + 2 * i + 4 * lh) =
+          *reinterpret_cast<u32x2*>(a.out + static_cast<int64_t>(row[g]) * D + 32 * t + 2 * i + 4 * lh) =
               u32x2{pack_bf16(o[t][g][i] * inv, o[t][g][i + 1] * inv), pack_bf16(o[t][g][i + 2] * inv, o[t][g][i + 3] * inv)};
     }
   }

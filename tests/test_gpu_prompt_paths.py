@@ -205,3 +205,29 @@ def test_new_tokens_of_nan_values(kind):
     out, lse = c.run(True)
     assert out[:200].isnan().all() and lse.isfinite().all()
     c.check(out, lse, True, [1])
+
+
+@pytest.mark.parametrize("kind", ["own", "bf16", "fp8"])
+def test_odd_values_take_a_few_times_as_long(kind):
+    """A request with such values may not hold up the others: both at most 20 times the finite call (4 was measured; one
+    column after the other, as it was once, 160)."""
+
+    def best(c):
+        c.run(True)
+        times = []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            c.run(True)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    c = Case(kind, [512], [2048], 8, 2, 128, 9)
+    finite = best(c)
+    c.put(0, 2048 - 250, 1, 7, NAN)
+    one = best(c)
+    for token in range(2048 - 512, 2048):
+        c.put(0, token, 0, slice(None), NAN)
+    assert one <= 20 * finite and best(c) <= 20 * finite
