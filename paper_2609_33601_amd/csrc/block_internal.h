@@ -94,6 +94,7 @@ hipError_t launch_paged_attention(const AttnArgs& a, hipStream_t st);
 
 // Attention of packed new tokens: over packed keys and values of their own, or over a paged cache.
 enum class PromptKv { kDense, kPagedBf16, kPagedFp8 };
+constexpr int64_t kPromptMaxSequences = 65536;  // a block's search for its own reaches 64 * 4096
 struct PromptArgs {
   const uint16_t* q;  // [T, Hq, D], tokens q_stride elements apart
   const void *k, *v;  // dense: [Tk, Hk, D] bf16, tokens k_stride, v_stride elements apart; else the cache

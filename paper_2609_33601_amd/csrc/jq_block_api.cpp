@@ -112,7 +112,7 @@ size_t attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Hq, int64_t Hk, 
 jq_status plan_prompt(int64_t T, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_len, bool paged, jq::PromptPlan* p) {
   if (T <= 0 || B <= 0 || Hq <= 0 || Hk <= 0 || max_len <= 0) return JQ_ERR_INVALID_ARG;
   if (Hq % Hk != 0 || (D != 64 && D != 128 && D != 256)) return JQ_ERR_UNSUPPORTED_SHAPE;
-  if (T > kMaxAxis || max_len > kMaxAxis || B > 65536 || Hq > 65536) return JQ_ERR_UNSUPPORTED_SHAPE;
+  if (T > kMaxAxis || max_len > kMaxAxis || B > jq::kPromptMaxSequences || Hq > 65536) return JQ_ERR_UNSUPPORTED_SHAPE;
   if (T * Hq >= (int64_t(1) << 31)) return JQ_ERR_UNSUPPORTED_SHAPE;
   *p = jq::prompt_plan(T, B, Hq, Hk, D, max_len, paged);
   // grids of fewer than 2^24 blocks of 256 threads (an 8-bit cache takes 128 columns where others take 256)

@@ -113,6 +113,7 @@ __device__ __forceinline__ Place find_tile(const PromptArgs& a, int G, int per, 
     // Sequence b has the places from starts[b] G / per + min(b, starts[b]) on, as
     // many as it needs or more, so a search finds it (4096 sequences of one token
     // over up to 64, 8 key heads: 350 us, by a walk along all sequences 960).
+    static_assert(kPromptMaxSequences <= 64 * 4096);
     for (int step = a.B > 4096 ? 4096 : 64; step > 1; step /= 64) {
       const int b = first + lane * step;
       const int start = b < a.B ? min(max(a.starts[b], 0), static_cast<int>(a.T)) : 0;
