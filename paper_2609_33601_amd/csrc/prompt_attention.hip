@@ -31,16 +31,18 @@
 // columns, would be half as many products again.
 //
 // What bounds it: a step's 32 MFMAs of a wave take 1024 cycles, its 117 vector
-// instructions and 32 exponentials 725, and of two waves' 3500 cycles a step takes
-// 3570: the matrix cores are busy for 57% of them, at 1.8 GHz (as long as one wave
-// on a SIMD issues less, it clocks at 2.3 and takes as long: power).  A fifth of
-// the vector instructions taken out gave 1 to 2%.  A large library product runs
-// at 1450 TFLOP/s on this card.  4608 tokens, 24 heads of 128, all of them seen:
-// 272 us, 960 TFLOP/s (864 equal blocks for 512 places); 8192 causal, 32 on 8
-// heads: 508, 1082; 2048 over 32768 cached: 965, 1105, and from e4m3 1155, whose
-// scales and widening are 130 more instructions a step.  Three prompts of up to
-// 77 tokens: 5.9 us, a launch and three steps' chain; 16 tokens over 2080: 12.4,
-// two launches.
+// instructions and 32 exponentials 725, and two waves' step takes 3570 for the 3500
+// that these sum to, so the two kinds hardly overlap: the matrix cores are busy for
+// 57% of a step, and by the counters for 51 to 57% of whole calls, at 1.75 to 1.9
+// GHz.  (One wave a SIMD, which issues less, clocked at 2.3 GHz and took as long,
+// and a fifth of the vector instructions taken out gave 1 to 2%, which points to
+// power; the power itself was not read.)  A large library product runs at 1450
+// TFLOP/s on this card.  4608 tokens, 24 heads of 128, all of them seen: 271 to 280
+// us from card to card, 930 to 960 TFLOP/s (864 equal blocks for 512 places); 8192
+// causal, 32 on 8 heads: 509, 1080; 2048 over 32768 cached: 965 to 1024, 1050 to
+// 1110, and from e4m3 1160 to 1180 us, whose scales and widening are 130 more
+// instructions a step.  Three prompts of up to 77 tokens: 6.0 us, a launch and two
+// steps' chain; 16 tokens over 2080: 12.6, two launches.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -409,7 +411,8 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QG, KV>::kPerSimd)) void prompt
   // Its part of the keys: every sequence is cut by its own length, so the bound
   // that the host knows decides only how many parts there may be.  The bounds go
   // to scalar registers by hand: left to itself the compiler works out a step's
-  // rows in vector ones (2048 tokens over 32768: 983 us instead of 965).
+  // rows in vector ones (2048 tokens over 32768, in turn on one card: 983 us
+  // instead of 965).
   const int chunk = parts == 1 ? nk : max(((nk - 1) / parts / 64 + 1) * 64, least);
   const int t_begin = __builtin_amdgcn_readfirstlane(min(static_cast<int64_t>(part) * chunk, static_cast<int64_t>(block_end)));
   const int t_end = __builtin_amdgcn_readfirstlane(min(block_end - t_begin, chunk) + t_begin);
