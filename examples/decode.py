@@ -191,6 +191,8 @@ def main():
     p.add_argument("--block", type=int, default=1, help="tokens of a step")
     p.add_argument("--cache", choices=("fp8", "bf16"), default="fp8")
     a = p.parse_args()
+    if a.prompt < 0 or a.chunk < 0:
+        p.error("--prompt and --chunk must not be negative")
     c = Config(cache=a.cache, head_norm=True, fused=True)
     tokens = a.prompt + (a.new + 1) * a.block
     decoder, cache = Decoder(c, tokens), Cache(c, a.batch, tokens)
@@ -198,9 +200,10 @@ def main():
 
     torch.cuda.synchronize()
     t = time.perf_counter()
-    chunk = a.chunk or a.prompt
+    longest = max(len(x) for x in prompts)
+    chunk = a.chunk or longest
     last = torch.zeros((a.batch, c.dim), dtype=torch.bfloat16, device="cuda")
-    for i in range(0, a.prompt, chunk):
+    for i in range(0, longest, chunk):
         y = decoder.extend([x[i: i + chunk] for x in prompts], cache)
         last = torch.where(torch.tensor([[i < len(x)] for x in prompts], device="cuda"), y, last)
     torch.cuda.synchronize()
